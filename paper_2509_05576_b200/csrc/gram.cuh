@@ -18,6 +18,7 @@
 // Every wait on an mbarrier is bounded; when one expires the CTA records PTQ_ERR_TIMEOUT, drains and returns.
 #pragma once
 #include "common.cuh"
+#include "tc.cuh"
 #include <utility>
 
 namespace ptq {
@@ -277,41 +278,8 @@ __global__ void __launch_bounds__(256) gram_split_conv_kernel(GramSource src, in
 }
 
 // ------------------------------------------------------------------------------------------------------------
-// PTX wrappers
+// int8 products
 // ------------------------------------------------------------------------------------------------------------
-// Bounded wait: gives up after about a second of polling or as soon as another thread of the CTA gave up.
-__device__ __forceinline__ bool mbar_wait_bounded(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-    const long long t0 = clock64();
-    uint32_t it = 0;
-    while (!mbar_try_wait(bar, parity)) {
-        if ((++it & 255u) == 0u) {
-            if (*abort_flag) return false;
-            if (clock64() - t0 > 2000000000LL) { *abort_flag = 1; return false; }
-        }
-    }
-    return true;
-}
-__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* tmap, int c0, int c1, int c2,
-                                            uint32_t bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-        ::"r"(dst), "l"(tmap), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
-        : "memory");
-}
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t (&r)[16]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-        : "r"(taddr));
-}
-__device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-
 // Shared-memory matrix descriptor of a K-major operand with 64-byte rows, SWIZZLE_64B, 8-row groups 512 bytes apart, as
 // two 32-bit words: the low one holds the start address / 16 (bits 0..13) and a leading offset that swizzled K-major
 // operands do not use, the high one the stride / 16, the descriptor version (bit 46) and the swizzle mode (bits 61..63).
