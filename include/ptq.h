@@ -239,6 +239,122 @@ size_t ptq_gemm_nt_sliced_workspace_bytes(int m, int n, int k);
 int ptq_gemm_nt_sliced(double *C, int64_t ldc, const double *A, int64_t lda, const double *B, int64_t ldb, int b_is_kn,
                        int m, int n, int k, double alpha, void *ws, size_t ws_bytes, int32_t *status, void *stream);
 
+/*
+ * ------------------------------------------------------------------------------------------------------------------
+ * Serving a quantized network: products in 8-bit floating point, and a key-value cache held in 4 bits.  The rules at the top of
+ * this file hold here too; what these calls add to them:
+ *   - `type` parameters name the element type of the caller's activations (ptq_type).
+ *   - Calls with nothing to do (no rows, no tokens) return PTQ_OK and launch nothing.
+ *   - Sizes that live on the device (lengths, offsets, page and slot numbers) are checked there: an entry that is out of range is
+ *     recorded in `status` (PTQ_ERR_INVALID_ARG, index = request or token) and is never used as an address.
+ * ------------------------------------------------------------------------------------------------------------------
+ */
+typedef enum { PTQ_F32 = 0, PTQ_F16 = 1, PTQ_BF16 = 2 } ptq_type;
+
+/*
+ * Casts a matrix to 8-bit floating point (e4m3: 3 fraction bits, largest magnitude 448) with one scale for each block of
+ * block_rows x 128 values (the last block of a row or column may be narrower):
+ *     scale = 2^e, e the least integer >= -126 with max |x| <= 448 2^e;    q = x / scale, rounded to nearest even.
+ * A power of two makes the quotient exact, so that a code is one rounding of x.
+ *   x       [rows x cols] of x_type, row stride ldx (16-byte loads are used where base and stride allow)
+ *   block_rows  1 (activations: a scale per row and 128 columns) or 128 (weights: a scale per 128 x 128)
+ *   q       [rows x cols] bytes, out, row stride ldq, a multiple of 16; bytes behind a row's last column are left as they are
+ *   scale   [ceil(rows / block_rows) x ceil(cols / 128)] float32, out, row stride ld_scale
+ * A NaN or an infinity is recorded in `status` (PTQ_ERR_NONFINITE, index = row, or first row of the block); its block's codes and
+ * scale become NaN, and with them what a product makes of that row (or of those columns).
+ */
+int ptq_fp8_quantize(const void *x, int x_type, int rows, int cols, int64_t ldx, int block_rows, uint8_t *q, int64_t ldq,
+                     float *scale, int64_t ld_scale, int32_t *status, void *stream);
+
+/*
+ * C = A B^T of operands in 8-bit floating point with block scales, as ptq_fp8_quantize makes them (any float32 scales are taken):
+ *     C[i][j] = sum_b scale_a[i][b] scale_b[j / 128][b] sum_{k in block b} A[i][k] B[j][k],    blocks of 128 along k
+ * Within a block the products are summed on the tensor cores, the blocks are joined in float32, and the result is rounded once to
+ * c_type.
+ *   C       [m x n] of c_type, out, row stride ldc
+ *   A       [m x k] bytes, row stride lda;  scale_a [m x ceil(k / 128)], row stride ld_scale_a
+ *   B       [n x k] bytes (a weight matrix as the layer stores it), row stride ldb;  scale_b [ceil(n / 128) x ceil(k / 128)]
+ *   lda, ldb: multiples of 16 (PTQ_ERR_ALIGNMENT otherwise); what lies behind a row's last column is not read
+ * Few rows (a decoded token) are bound by the one read of B; no workspace.  Beyond m = 2^20 or n = 2^22: PTQ_ERR_UNSUPPORTED.
+ */
+int ptq_fp8_matmul(void *C, int c_type, int64_t ldc, const uint8_t *A, int64_t lda, const float *scale_a, int64_t ld_scale_a,
+                   const uint8_t *B, int64_t ldb, const float *scale_b, int64_t ld_scale_b, int m, int n, int k, int32_t *status,
+                   void *stream);
+
+/*
+ * The cache: pages[num_pages][kv_heads][page_size / 16] tiles of 16 tokens.  A tile holds, for one key-value head,
+ *     K codes [16][head_dim / 2], K grids [16][head_dim / 32] uint16, V codes, V grids
+ * with two 4-bit codes a byte (the even value in the low half).  Every 32 values share a min-max grid whose range contains 0, as
+ * the rows of ptq_minmax_grid do: with lo = min(0, min), hi = max(0, max),
+ *     s = the least fp16 number of 6 significant bits >= (hi - lo) / 15, within [2^-19, 2112];   z = clamp(rint(-lo / s), 0, 15)
+ *     code = clamp(rint(x / s) + z, 0, 15), held value = s (code - z)
+ * and the grid's 16 bits are the fp16 pattern of s (whose low five bits are 0) with z in the lowest four.  A held value has at
+ * most ten significant bits, so it is an fp16 number and nothing is rounded when it is used; magnitudes beyond 15 x 2112 saturate.
+ * 4.5 bits a value: 144 bytes for a token's key and value in a head of 128.
+ *   page_size  16, 32, 64, 128, 256, 512 or 1024 tokens;  head_dim  64 or 128 (PTQ_ERR_UNSUPPORTED otherwise)
+ * ptq_cache_page_bytes: the size of one page, 0 for what is not supported (host function, no CUDA calls).  A token's slot is
+ * page * page_size + its place in the page; num_pages * page_size <= 2^31 - 1.
+ */
+size_t ptq_cache_page_bytes(int page_size, int kv_heads, int head_dim);
+
+/*
+ * Where the new tokens of a batch of requests go: extends the requests' block tables by pages of the free list and lists slot and
+ * position of every new token, in one launch.
+ *   kv_lens     [batch] int32: tokens cached of each request;  new_tokens [batch] int32: how many are added (0 is fine)
+ *   block_table [batch x max_pages] int32, in/out, row stride ld_table: the pages of each request in order.  The entries of pages
+ *               that hold cached tokens are read, those of pages that begin with a new token are written, others stay.
+ *   free_pages  [num_free] int32: pages are taken from its front, in the order of the requests and of their pages
+ *   slots       [max_tokens] int32, out;  positions [max_tokens] int32, out: of the new tokens of request 0, then 1, ...; -1 in both
+ *               behind the last token, which ptq_cache_append skips (a batch padded to a fixed size, as a captured graph needs it)
+ *   cu_q        [batch + 1] int32, out: first new token of each request, and their number
+ *   kv_lens_out [batch] int32, out: kv_lens + new_tokens; must not overlap kv_lens (PTQ_ERR_INVALID_ARG)
+ *   taken       [1] int32, out: pages taken from the free list
+ * If a request does not fit (its table row, max_tokens, num_free, a negative length), status gets PTQ_ERR_INVALID_ARG with the
+ * first such request, and nothing is done for any: slots and positions are all -1, cu_q all 0, kv_lens_out = kv_lens, taken 0 and
+ * the table as it was.
+ */
+int ptq_cache_plan(const int32_t *kv_lens, const int32_t *new_tokens, int batch, int page_size, int32_t *block_table,
+                   int64_t ld_table, int max_pages, const int32_t *free_pages, int num_free, int32_t *slots, int32_t *positions,
+                   int max_tokens, int32_t *cu_q, int32_t *kv_lens_out, int32_t *taken, int32_t *status, void *stream);
+
+/*
+ * Writes keys and values of tokens into the cache.
+ *   k, v   [tokens][kv_heads][head_dim] of `type`; strides between tokens and between heads in elements, a head's values contiguous
+ *   slots  [tokens] int32; a negative slot is skipped.  The slots of one call differ from one another.
+ * A NaN is held as 0, an infinity as the end of its group's grid; both are recorded (PTQ_ERR_NONFINITE, index = token), and the
+ * cache itself stays finite.
+ */
+int ptq_cache_append(void *pages, int num_pages, int page_size, int kv_heads, int head_dim, const void *k, int64_t k_token,
+                     int64_t k_head, const void *v, int64_t v_token, int64_t v_head, int type, const int32_t *slots, int tokens,
+                     int32_t *status, void *stream);
+
+/* The values that the cache holds at `slots`, to k and v (as above, written); rows of negative slots are left as they are. */
+int ptq_cache_read(const void *pages, int num_pages, int page_size, int kv_heads, int head_dim, void *k, int64_t k_token,
+                   int64_t k_head, void *v, int64_t v_token, int64_t v_head, int type, const int32_t *slots, int tokens,
+                   int32_t *status, void *stream);
+
+/*
+ * Attention of the newest tokens of a batch of requests over what is cached of them, themselves included.  Request r has the rows
+ * cu_q[r] .. cu_q[r + 1] - 1 of q, the last of its kv_lens[r] tokens; with n of them, row i stands at position p = kv_lens[r] - n + i
+ * and sees the keys j < kv_lens[r] with j <= p (causal) and j > p - window (window > 0):
+ *     out = sum_j softmax_j(scale q . k_j) v_j,     lse = log sum_j exp(scale q . k_j)
+ * A row that sees no key gets out = 0 and lse = -infinity.  Query head h reads key-value head h / (q_heads / kv_heads).
+ *   q, out  [total_q][q_heads][head_dim] of `type` (PTQ_F16 or PTQ_BF16), strides between tokens and heads in elements; the cache is
+ *           read as fp16 either way, and bf16 queries are brought to fp16 by a power of two for each row, which loses nothing
+ *   lse     [total_q][q_heads] float32, or NULL
+ *   block_table, kv_lens, cu_q: as ptq_cache_plan leaves them (kv_lens_out).  Rows behind cu_q[batch] are left as they are.
+ *   max_q   the most rows that any request has (it chooses kernels and the workspace; any bound is right, a tight one is fast)
+ * Scores, their maximum and sum, and the output are held in float32; the probabilities enter the second product as fp16.
+ * Workspace: ptq_cache_attention_workspace_bytes(q_heads, kv_heads, head_dim, max_q) (host function, no CUDA calls); it depends on
+ * max_q alone where the other three are given, not on lengths.  Results do not depend on what else runs.
+ */
+size_t ptq_cache_attention_workspace_bytes(int q_heads, int kv_heads, int head_dim, int max_q);
+int ptq_cache_attention(void *out, int64_t o_token, int64_t o_head, float *lse, const void *q, int64_t q_token, int64_t q_head,
+                        int type, int q_heads, const void *pages, int num_pages, int page_size, int kv_heads, int head_dim,
+                        const int32_t *block_table, int64_t ld_table, int max_pages, const int32_t *kv_lens, const int32_t *cu_q,
+                        int batch, int total_q, int max_q, float scale, int causal, int window, void *ws, size_t ws_bytes,
+                        int32_t *status, void *stream);
+
 const char *ptq_status_string(int code);
 int ptq_version(void);
 

@@ -1,0 +1,809 @@
+// A key-value cache held in 4 bits: where its tokens go, writing and reading it, and attention of a few rows over it.
+//
+// Grid: every 32 values of a key or value share a min-max grid with 0 in its range, as the rows of a weight matrix do
+// (ptq_minmax_grid).  Its step s is rounded UP to a number of 6 significant bits, so that s (c - z) with 4-bit codes has at most ten
+// and is exactly an fp16 number: what the tensor cores multiply is what the cache stands for, and no product rounds an operand.
+// Step and zero code share 16 bits: the fp16 pattern of s, whose low five bits are zero, with z in the lowest four.
+//
+// Layout: pages[page][kv_head][tile of 16 tokens][K codes | K grids | V codes | V grids], so that one tile of one head is one
+// contiguous piece (2304 bytes for heads of 128) and comes in one bulk copy.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+#include "fp8.cuh"
+#include "tc.cuh"
+
+namespace ptq {
+
+constexpr int kC4Tile = 16, kC4Group = 32;
+constexpr float kC4MinStep = 1.9073486328125e-06f, kC4MaxStep = 2112.0f;     // 2^-19; 33 2^6: (16 + z) s and 16 s stay below 65504
+
+__host__ __device__ constexpr int c4_side_bytes(int dim) { return kC4Tile * (dim / 2 + dim / kC4Group * 2); }
+__host__ __device__ constexpr int c4_tile_bytes(int dim) { return 2 * c4_side_bytes(dim); }
+
+struct Cache4 {
+    uint8_t* pages;
+    int num_pages, page_shift, kv_heads;       // page size = 1 << page_shift
+};
+template <int HD>
+__device__ __forceinline__ uint8_t* c4_tile(const Cache4& c, int page, int head, int tile) {
+    const int per = 1 << (c.page_shift - 4);
+    return c.pages + (((int64_t)page * c.kv_heads + head) * per + tile) * c4_tile_bytes(HD);
+}
+
+// ------------------------------------------------------------------------------------------------------------
+// Block tables and slots
+// ------------------------------------------------------------------------------------------------------------
+struct CachePlan {
+    const int32_t* lens;          // [batch] tokens cached before
+    const int32_t* fresh;         // [batch] new tokens
+    int batch;
+    int32_t* table;               // [batch][max_pages], in/out
+    int64_t ldt;
+    int max_pages;
+    const int32_t* free_pages;
+    int num_free, page_shift;
+    int32_t* slots;               // [max_tokens]
+    int32_t* positions;           // [max_tokens]
+    int max_tokens;
+    int32_t* cu;                  // [batch + 1]
+    int32_t* lens_out;            // [batch]
+    int32_t* taken;               // [1]
+    int32_t* status;
+};
+
+constexpr int kPlanThreads = 1024, kPlanTokens = 4096;       // threads a CTA; tokens a CTA answers for
+
+// Sums of (tokens, pages) over the CTA's threads before this one; totals in `all`.  One pair in 64 bits: tokens may reach 2^31
+// (checked in 64 bits by the caller), so the two are scanned apart.
+__device__ __forceinline__ longlong2 plan_scan(longlong2 v, longlong2* warp_sums, longlong2& all) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    longlong2 x = v;
+#pragma unroll
+    for (int s = 1; s < 32; s <<= 1) {
+        const long long a = __shfl_up_sync(0xffffffffu, x.x, s), b = __shfl_up_sync(0xffffffffu, x.y, s);
+        if (lane >= s) { x.x += a; x.y += b; }
+    }
+    __syncthreads();
+    if (lane == 31) warp_sums[warp] = x;
+    __syncthreads();
+    if (warp == 0) {
+        longlong2 w = warp_sums[lane];
+#pragma unroll
+        for (int s = 1; s < 32; s <<= 1) {
+            const long long a = __shfl_up_sync(0xffffffffu, w.x, s), b = __shfl_up_sync(0xffffffffu, w.y, s);
+            if (lane >= s) { w.x += a; w.y += b; }
+        }
+        warp_sums[lane] = w;
+    }
+    __syncthreads();
+    all = warp_sums[31];
+    const longlong2 before = warp ? warp_sums[warp - 1] : make_longlong2(0, 0);
+    return make_longlong2(before.x + x.x - v.x, before.y + x.y - v.y);
+}
+
+// One launch.  Every CTA scans all requests (a thousand at a time) and answers for kPlanTokens tokens; the first one also writes
+// what belongs to requests.  Nothing is written before the whole batch is known to fit: a batch that does not leaves every slot at
+// -1, no rows (cu = 0), the lengths as they were and the table untouched.  A new page's first token is always new, so that the
+// token writes the page's table entry.
+__global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(CachePlan p) {
+    chained_begin();
+    __shared__ longlong2 warp_sums[32];
+    __shared__ int bad_request;
+    const int lane = threadIdx.x & 31, ps = 1 << p.page_shift;
+    const long long t0 = (long long)blockIdx.x * kPlanTokens, t1 = t0 + kPlanTokens;
+    if (threadIdx.x == 0) bad_request = 0x7fffffff;
+    __syncthreads();
+    auto request = [&](int b, int& len, int& n, int& have, int& want) {
+        len = n = have = want = 0;
+        if (b >= p.batch) return true;
+        len = p.lens[b];
+        n = p.fresh[b];
+        if (len < 0 || n < 0 || (long long)len + n > 0x7fffffffll - ps) { len = n = 0; return false; }
+        have = (len + ps - 1) >> p.page_shift;
+        want = (len + n + ps - 1) >> p.page_shift;
+        return want <= p.max_pages;
+    };
+    long long tokens = 0, pages = 0;
+    for (int first = 0; first < p.batch; first += kPlanThreads) {
+        int len, n, have, want;
+        const int b = first + threadIdx.x;
+        const bool ok = request(b, len, n, have, want);
+        longlong2 all;
+        const longlong2 at = plan_scan(make_longlong2(n, want - have), warp_sums, all);
+        if (b < p.batch && (!ok || tokens + at.x + n > p.max_tokens || pages + at.y + want - have > p.num_free)) atomicMin(&bad_request, b);
+        tokens += all.x;
+        pages += all.y;
+    }
+    __syncthreads();
+    const int bad = bad_request;
+    const bool fits = bad == 0x7fffffff;
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        p.cu[0] = 0;
+        p.taken[0] = fits ? (int)pages : 0;
+        if (!fits) report(p.status, PTQ_ERR_INVALID_ARG, bad);
+    }
+    const long long used = fits ? tokens : 0;
+    for (long long t = t0 + threadIdx.x; t < t1 && t < p.max_tokens; t += kPlanThreads)
+        if (t >= used) { p.slots[t] = -1; p.positions[t] = -1; }
+    if (!fits) {
+        if (blockIdx.x == 0)
+            for (int b = threadIdx.x; b < p.batch; b += kPlanThreads) { p.cu[b + 1] = 0; p.lens_out[b] = p.lens[b]; }
+        return;
+    }
+    tokens = pages = 0;
+    for (int first = 0; first < p.batch; first += kPlanThreads) {
+        int len, n, have, want;
+        const int b = first + threadIdx.x;
+        request(b, len, n, have, want);
+        longlong2 all;
+        longlong2 at = plan_scan(make_longlong2(n, want - have), warp_sums, all);
+        at.x += tokens;
+        at.y += pages;
+        tokens += all.x;
+        pages += all.y;
+        if (b < p.batch && blockIdx.x == 0) { p.cu[b + 1] = (int)(at.x + n); p.lens_out[b] = len + n; }
+        // the warp takes the requests of its lanes that have tokens here one after the other, 32 tokens at a time; where each
+        // has one token only, every lane takes its own
+        const bool mine = n > 0 && at.x < t1 && at.x + n > t0;
+        const bool single = __all_sync(0xffffffffu, n <= 1);
+        unsigned todo = __ballot_sync(0xffffffffu, mine);
+        if (single && !mine) todo = 0;
+        if (single && mine) todo = 1u << lane;
+        while (todo) {
+            const int src = __ffs(todo) - 1;
+            todo &= todo - 1;
+            int rb = b, rlen = len, rn = n, rhave = have, rat = (int)at.x, rpage = (int)at.y;
+            if (!single) {
+                rb = __shfl_sync(0xffffffffu, b, src); rlen = __shfl_sync(0xffffffffu, len, src);
+                rn = __shfl_sync(0xffffffffu, n, src); rhave = __shfl_sync(0xffffffffu, have, src);
+                rat = __shfl_sync(0xffffffffu, (int)at.x, src); rpage = __shfl_sync(0xffffffffu, (int)at.y, src);
+            }
+            int32_t* row = p.table + (int64_t)rb * p.ldt;
+            const int lo = t0 > rat ? (int)(t0 - rat) : 0, hi = t1 < (long long)rat + rn ? (int)(t1 - rat) : rn;
+            for (int i = lo + (single ? 0 : lane); i < hi; i += single ? 1 : 32) {
+                const int pos = rlen + i, pi = pos >> p.page_shift;
+                const int page = pi >= rhave ? p.free_pages[rpage + pi - rhave] : row[pi];
+                if (pi >= rhave && (pos & (ps - 1)) == 0) row[pi] = page;
+                const long long slot = ((long long)page << p.page_shift) + (pos & (ps - 1));
+                const bool ok = page >= 0 && slot <= 0x7fffffffll;
+                if (!ok) report(p.status, PTQ_ERR_INVALID_ARG, rb, 1);
+                p.slots[rat + i] = ok ? (int)slot : -1;
+                p.positions[rat + i] = pos;
+            }
+        }
+        __syncwarp();
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------------
+// Writing and reading
+// ------------------------------------------------------------------------------------------------------------
+// Step of a group with extremes lo <= 0 <= hi: (hi - lo) / 15 rounded up to 6 significant bits, as an fp16 pattern.
+__device__ __forceinline__ uint32_t c4_step_bits(float lo, float hi) {
+    const float r = fminf((hi - lo) / 15.0f, kC4MaxStep);
+    const uint32_t h = __half_as_ushort(__float2half_ru(r));
+    const uint32_t up = (h + 31u) & ~31u;
+    return up < 32u ? 32u : up;                        // 32 is the pattern of 2^-19
+}
+
+struct C4Tokens {
+    void* k;
+    void* v;
+    int64_t k_token, k_head, v_token, v_head;          // strides in elements; the head's values are contiguous
+    const int32_t* slots;
+    int tokens, vec;                                   // vec: every row begins on 16 bytes
+    int32_t* status;
+};
+
+// Eight values a thread, four threads a group.  Bound by memory, or by its launch: a step of decoding writes a few hundred rows.
+// A NaN is held as 0 and an infinity as the end of the grid (both recorded in status): the cache itself stays finite, so that a
+// masked token can never reach a sum.
+template <typename T, int HD>
+__global__ void __launch_bounds__(256) cache_append_kernel(Cache4 c, C4Tokens a) {
+    chained_begin();
+    constexpr int kRow = HD / 8;                                    // threads a row
+    const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x, row = u / kRow;
+    const int sub = (int)(u - row * kRow);
+    const int64_t th = row >> 1;
+    const int token = (int)(th / c.kv_heads), head = (int)(th - (int64_t)token * c.kv_heads), side = (int)(row & 1);
+    int slot = token < a.tokens ? a.slots[token] : -1;
+    if (slot >= 0 && (slot >> c.page_shift) >= c.num_pages) {
+        if (sub == 0) report(a.status, PTQ_ERR_INVALID_ARG, token);
+        slot = -1;
+    }
+    float v[8];
+    const T* src = side ? static_cast<const T*>(a.v) + token * a.v_token + head * a.v_head
+                        : static_cast<const T*>(a.k) + token * a.k_token + head * a.k_head;
+    load8<T>(src + sub * 8, slot >= 0 ? 8 : 0, a.vec, v);
+    float lo = 0.f, hi = 0.f;
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        bad |= not_finite(v[i]);
+        if (v[i] != v[i]) v[i] = 0.f;
+        lo = fminf(lo, v[i]);
+        hi = fmaxf(hi, v[i]);
+    }
+#pragma unroll
+    for (int s = 1; s < 4; s <<= 1) {
+        lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, s));
+        hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, s));
+    }
+    if (slot < 0) return;
+    if (bad) report(a.status, PTQ_ERR_NONFINITE, token);
+    const uint32_t bits = c4_step_bits(lo, hi);
+    const float step = __half2float(__ushort_as_half((unsigned short)bits));
+    // true divisions: a tie between two codes is then a tie in any precision, and goes to the even one
+    const float zero = fminf(fmaxf(rintf(-lo / step), 0.f), 15.f);
+    uint32_t codes = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float code = fminf(fmaxf(rintf(v[i] / step) + zero, 0.f), 15.f);
+        codes |= (uint32_t)code << (4 * i);
+    }
+    const int in_page = slot & ((1 << c.page_shift) - 1), r = in_page & (kC4Tile - 1);
+    uint8_t* tile = c4_tile<HD>(c, slot >> c.page_shift, head, in_page >> 4) + side * c4_side_bytes(HD);
+    *reinterpret_cast<uint32_t*>(tile + r * (HD / 2) + sub * 4) = codes;
+    if ((sub & 3) == 0)
+        *reinterpret_cast<uint16_t*>(tile + kC4Tile * (HD / 2) + (r * (HD / kC4Group) + (sub >> 2)) * 2) = (uint16_t)(bits | (uint32_t)zero);
+}
+
+template <typename T, int HD>
+__global__ void __launch_bounds__(256) cache_read_kernel(Cache4 c, C4Tokens a) {
+    chained_begin();
+    constexpr int kRow = HD / 8;
+    const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x, row = u / kRow;
+    const int sub = (int)(u - row * kRow);
+    const int64_t th = row >> 1;
+    const int token = (int)(th / c.kv_heads), head = (int)(th - (int64_t)token * c.kv_heads), side = (int)(row & 1);
+    const int slot = token < a.tokens ? a.slots[token] : -1;
+    if (slot < 0) return;
+    if ((slot >> c.page_shift) >= c.num_pages) {
+        if (sub == 0) report(a.status, PTQ_ERR_INVALID_ARG, token);
+        return;
+    }
+    const int in_page = slot & ((1 << c.page_shift) - 1), r = in_page & (kC4Tile - 1);
+    const uint8_t* tile = c4_tile<HD>(c, slot >> c.page_shift, head, in_page >> 4) + side * c4_side_bytes(HD);
+    const uint32_t codes = *reinterpret_cast<const uint32_t*>(tile + r * (HD / 2) + sub * 4);
+    const uint32_t word = *reinterpret_cast<const uint16_t*>(tile + kC4Tile * (HD / 2) + (r * (HD / kC4Group) + (sub >> 2)) * 2);
+    const float step = __half2float(__ushort_as_half((unsigned short)(word & 0xffe0u)));
+    const int zero = (int)(word & 15u);
+    alignas(16) T out[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) out[i] = from_f32<T>(step * (float)((int)(codes >> (4 * i) & 15u) - zero));
+    T* dst = side ? static_cast<T*>(a.v) + token * a.v_token + head * a.v_head : static_cast<T*>(a.k) + token * a.k_token + head * a.k_head;
+    dst += sub * 8;
+    if (a.vec) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(dst)[i] = reinterpret_cast<const uint4*>(out)[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dst[i] = out[i];
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------------
+// Attention
+// ------------------------------------------------------------------------------------------------------------
+struct Attn4 {
+    Cache4 cache;
+    const void* q;
+    void* out;
+    float* lse;                                   // [total_q][q_heads] or NULL
+    int64_t q_token, q_head, o_token, o_head;     // strides in elements
+    const int32_t* table;
+    int64_t ldt;
+    int max_pages;
+    const int32_t* lens;                          // [batch] tokens cached, the new ones among them
+    const int32_t* cu;                            // [batch + 1] first row of each request
+    int batch, total_q, q_heads, ratio;           // ratio = q_heads / kv_heads
+    float scale_log2;                             // scale log2(e)
+    int causal, window;
+    int row_limit;                                // requests with more rows (new tokens x ratio) than this are left to the other kernel
+    float* partial;
+    int32_t* status;
+};
+
+struct AttnRequest {
+    int row0, n, len, rows, tiles, chunk0, chunks;       // tiles of kRows rows; 32- or 64-token chunks from chunk0 on
+    long long units;
+};
+
+template <int kRows, int kChunk>
+__device__ __forceinline__ AttnRequest attn_request(const Attn4& a, int b) {
+    AttnRequest r;
+    const int c0 = a.cu[b], c1 = a.cu[b + 1], len = a.lens[b], most = a.max_pages << a.cache.page_shift;
+    r.row0 = min(max(c0, 0), a.total_q);
+    r.n = max(min(max(c1, 0), a.total_q) - r.row0, 0);
+    r.len = min(max(len, 0), most);
+    if (c0 != r.row0 || c1 != r.row0 + r.n || len != r.len) report(a.status, PTQ_ERR_INVALID_ARG, b);
+    r.rows = r.n * a.ratio;
+    if (r.rows > a.row_limit) r.rows = 0;
+    r.tiles = (r.rows + kRows - 1) / kRows;
+    const int low = a.window > 0 ? min(max((long long)r.len - r.n - a.window + 1, 0ll), (long long)r.len) : 0;
+    r.chunk0 = low / kChunk;
+    r.chunks = max((r.len + kChunk - 1) / kChunk - r.chunk0, 1);          // a request without keys still has rows to write
+    r.units = (long long)a.cache.kv_heads * r.tiles * r.chunks;
+    return r;
+}
+// Keys [lo, hi) that row token i of the request sees.
+__device__ __forceinline__ void attn_range(const Attn4& a, const AttnRequest& r, int i, int& lo, int& hi) {
+    const int pos = r.len - r.n + i;
+    hi = a.causal ? min(max(pos + 1, 0), r.len) : r.len;
+    lo = a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0;
+}
+
+// Step and zero code of two 16-bit grid words to the factors that unpack their codes: with h = 1 + c / 16 (a nibble set into the
+// mantissa of 1.0), s (c - z) = 16 s h - (16 + z) s.  16 s and (16 + z) s are exact in fp16 (6 and 11 significant bits), the
+// difference has at most ten: the fused multiply-add rounds nothing.
+struct C4Factors { __half2 step16, off; };
+__device__ __forceinline__ C4Factors c4_factors(uint32_t words) {
+    const uint32_t s = words & 0xffe0ffe0u, z = ((words & 0x000f000fu) << 6) | 0x4c004c00u;       // 16 + z
+    const __half2 step = *reinterpret_cast<const __half2*>(&s), zero = *reinterpret_cast<const __half2*>(&z);
+    C4Factors f;
+    f.step16 = __hmul2(step, __float2half2_rn(16.f));
+    f.off = __hneg2(__hmul2(step, zero));
+    return f;
+}
+// Nibbles i of both halves of x, i = 0 .. 3.
+__device__ __forceinline__ void c4_unpack4(uint32_t x, const C4Factors& f, uint32_t (&o)[4]) {
+    const uint32_t h[4] = {((x << 6) & 0x03c003c0u) | 0x3c003c00u, ((x << 2) & 0x03c003c0u) | 0x3c003c00u,
+                           ((x >> 2) & 0x03c003c0u) | 0x3c003c00u, ((x >> 6) & 0x03c003c0u) | 0x3c003c00u};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __half2 v = __hfma2(*reinterpret_cast<const __half2*>(&h[i]), f.step16, f.off);
+        o[i] = *reinterpret_cast<const uint32_t*>(&v);
+    }
+}
+
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    return r;
+}
+__device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float exp2_approx(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// Power of two that brings a row of queries whose largest magnitude is `top` to [2^14, 2^15), so that bf16 queries become fp16
+// ones without loss (what lies 2^-38 below the row's largest is flushed); 1 for rows of zeros and for those that are not finite.
+__device__ __forceinline__ int attn_q_shift(float top) {
+    if (top == 0.f || not_finite(top)) return 0;
+    return min(14 - ((int)(__float_as_uint(top) >> 23) - 127), 126);
+}
+
+// Probabilities are kept times 2^15 in fp16: down to 2^-29 of the largest they keep all their bits, and nothing above 2^-39 of it
+// is lost, so that many small ones still add up.
+constexpr float kAttnPShift = 15.f;
+
+template <typename T> constexpr bool kIsHalf = false;
+template <> constexpr bool kIsHalf<__half> = true;
+
+constexpr int kFewWarps = 8, kFewStages = 3, kFewMaxCtas = 320;
+template <int HD> struct FewShape {
+    static constexpr int tiles = HD == 128 ? 2 : 4;                   // tiles of a chunk: 4608 bytes either way
+    static constexpr int chunk = tiles * kC4Tile;
+    static constexpr int chunk_bytes = tiles * c4_tile_bytes(HD);
+    static constexpr int ring_bytes = kFewWarps * kFewStages * chunk_bytes;
+    static constexpr int smem_bytes = ring_bytes + 1024;
+};
+__host__ __device__ constexpr int few_partial_floats(int hd, int nt) { return 8 * nt * (hd + 2); }
+
+// The units of all requests are dealt to the CTAs in equal shares, in the order (request, kv head, row tile, chunk): a long request
+// and a batch of short ones fill the GPU alike.  A CTA finds its share by adding up the requests' units, 256 at a time.
+constexpr int kFewThreads = 32 * kFewWarps;
+struct FewScan { long long warp[kFewWarps]; long long before; int b; };
+template <int kRows, int kChunk>
+__device__ __forceinline__ long long few_total(const Attn4& a, FewScan& s) {
+    long long mine = 0;
+    for (int b = threadIdx.x; b < a.batch; b += kFewThreads) mine += attn_request<kRows, kChunk>(a, b).units;
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, d);
+    if ((threadIdx.x & 31) == 0) s.warp[threadIdx.x >> 5] = mine;
+    __syncthreads();
+    long long total = 0;
+#pragma unroll
+    for (int w = 0; w < kFewWarps; ++w) total += s.warp[w];
+    __syncthreads();
+    return total;
+}
+// Sum of v over the threads before this one; `all`: over all of them.
+__device__ __forceinline__ long long few_scan(long long v, FewScan& s, long long& all) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    long long x = v;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const long long y = __shfl_up_sync(0xffffffffu, x, d);
+        if (lane >= d) x += y;
+    }
+    if (lane == 31) s.warp[warp] = x;
+    __syncthreads();
+    all = 0;
+    long long before = 0;
+#pragma unroll
+    for (int w = 0; w < kFewWarps; ++w) {
+        if (w == warp) before = all;
+        all += s.warp[w];
+    }
+    __syncthreads();
+    return before + x - v;
+}
+__device__ __forceinline__ long long few_share(long long total, int ctas) {
+    const long long even = (total + ctas - 1) / ctas;
+    return even < kFewWarps ? kFewWarps : even;          // less than a chunk a warp would only add partial results
+}
+
+// Few rows (the new tokens of a request times the query heads of a kv head, up to 8 NT): what counts is one read of the cache.
+// A warp takes every eighth chunk of the CTA's share and keeps three of them in flight (bulk copies, 4608 bytes each; sixteen
+// warps an SM).  The cache is the 16-row operand of the tensor cores and the query rows their eight columns, so that a group of up to
+// eight query heads costs half of what it would the other way round:  S^T = K q (16 tokens x 8 rows), O^T = V^T P^T (16 values x
+// 8 rows).  Codes go from shared memory to registers as they lie and become fp16 there: three instructions for two values.
+// The order of a contraction is free, so the four lanes that share a token take 32 consecutive values each, and q is laid out alike.
+template <typename T, int HD, int NT>
+__global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) attn4_few_kernel(Attn4 a) {
+    using F = FewShape<HD>;
+    constexpr int kRows = 8 * NT, kWords = HD / 32, kSteps = HD / 16, kTiles = HD / 16;
+    constexpr int kSide = c4_side_bytes(HD), kTileBytes = c4_tile_bytes(HD), kCodes = kC4Tile * HD / 2, kGrids = HD / kC4Group * 2;
+    extern __shared__ unsigned char few_smem_raw[];
+    __shared__ FewScan scan;
+    __shared__ uint64_t bars[kFewWarps * kFewStages];
+    __shared__ float stat_m[kFewWarps][kRows], stat_l[kFewWarps][kRows];
+    __shared__ int abort_word;
+    unsigned char* ring = few_smem_raw + (1024 - (smem_u32(few_smem_raw) & 1023)) % 1024;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n8 = lane >> 2, t = lane & 3;
+    const uint32_t ring_w = smem_u32(ring) + warp * kFewStages * F::chunk_bytes;
+    const unsigned char* ring_p = ring + warp * kFewStages * F::chunk_bytes;
+    const uint32_t bar_w = smem_u32(&bars[warp * kFewStages]);
+    if (lane < kFewStages) mbar_init(bar_w + 8 * lane, 1);
+    if (threadIdx.x == 0) { scan.b = 0; scan.before = 0; abort_word = 0; }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncthreads();
+    chained_begin();
+
+    const long long total = few_total<kRows, F::chunk>(a, scan), share = few_share(total, gridDim.x);
+    long long u = share * blockIdx.x;
+    const long long u_end = min(u + share, total);
+    if (u >= total) return;
+    for (long long base = 0, first = 0; first < a.batch; first += kFewThreads) {
+        const int b = (int)first + threadIdx.x;
+        const long long mine = b < a.batch ? attn_request<kRows, F::chunk>(a, b).units : 0;
+        long long all;
+        const long long before = base + few_scan(mine, scan, all);
+        if (before <= u && u < before + mine) { scan.b = b; scan.before = before; }
+        base += all;
+        if (base > u) break;
+    }
+    __syncthreads();
+    int b = scan.b;
+    long long before = scan.before;
+    unsigned uses = 0;                                   // chunks this warp has asked for so far, over all pieces
+    unsigned done = 0;
+
+    while (u < u_end) {
+        AttnRequest r = attn_request<kRows, F::chunk>(a, b);
+        while (u >= before + r.units) { before += r.units; ++b; r = attn_request<kRows, F::chunk>(a, b); }
+        const int seg = (int)((u - before) / r.chunks), from = (int)((u - before) - (long long)seg * r.chunks);
+        const int head = seg / r.tiles, tile = seg - head * r.tiles;
+        const int to = (int)min((long long)r.chunks, from + (u_end - u));
+        u += to - from;
+        const int first_row = tile * kRows, live_rows = min(kRows, r.rows - first_row);
+        // keys that any row, and that every row of the tile sees
+        int lo_any, hi_any, lo_all, hi_all;
+        attn_range(a, r, first_row / a.ratio, lo_any, hi_all);           // rows that do not exist may compute anything: nobody reads them
+        attn_range(a, r, (first_row + live_rows - 1) / a.ratio, lo_all, hi_any);
+        const int c_first = max(r.chunk0 + from, lo_any / F::chunk), c_last = min(r.chunk0 + to, (hi_any + F::chunk - 1) / F::chunk);
+
+        // the query rows, in the order in which the codes come
+        uint32_t qf[NT][kSteps][2];
+        float mult[NT][2];
+        int lo[NT][2], hi[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int row = first_row + nt * 8 + n8;
+            float v[8 * kWords], top = 0.f;
+            const bool live = row < r.rows;
+            const int i = live ? row / a.ratio : 0;
+            const T* q = static_cast<const T*>(a.q) + (int64_t)(r.row0 + i) * a.q_token + (int64_t)(head * a.ratio + (live ? row - i * a.ratio : 0)) * a.q_head;
+#pragma unroll
+            for (int j = 0; j < 8 * kWords; ++j) { v[j] = live ? to_f32<T>(q[t * 8 * kWords + j]) : 0.f; top = fmaxf(top, fabsf(v[j])); if (not_finite(v[j])) top = __uint_as_float(0x7f800000u); }
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            const int shift = sizeof(T) == 2 && !kIsHalf<T> ? attn_q_shift(top) : 0;
+            const float f = exp2_int(shift);
+#pragma unroll
+            for (int w = 0; w < kWords; ++w)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float* x = v + 8 * w + 2 * h;
+                    qf[nt][2 * w + h][0] = pack_half2(x[0] * f, x[4] * f);
+                    qf[nt][2 * w + h][1] = pack_half2(x[1] * f, x[5] * f);
+                }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int rr = first_row + nt * 8 + 2 * t + h;
+                mult[nt][h] = a.scale_log2 * exp2_int(-__shfl_sync(0xffffffffu, shift, (2 * t + h) * 4));
+                lo[nt][h] = hi[nt][h] = 0;
+                if (rr < r.rows) attn_range(a, r, rr / a.ratio, lo[nt][h], hi[nt][h]);
+            }
+        }
+
+        float m[NT][2], l[NT][2], o[NT][kTiles][4];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) { m[nt][h] = -INFINITY; l[nt][h] = 0.f; }
+#pragma unroll
+            for (int j = 0; j < kTiles; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[nt][j][e] = 0.f;
+        }
+        const int last_tile = (hi_any + kC4Tile - 1) / kC4Tile;
+        auto ask = [&](int c) {                          // the tiles of chunk c that hold keys; the whole warp
+            const int stage = uses % kFewStages, tile0 = c * F::tiles, count = min(F::tiles, last_tile - tile0);
+            const uint32_t bar = bar_w + 8 * stage;
+            if (lane == 0) mbar_arrive_expect_tx(bar, count * kTileBytes);
+            __syncwarp();
+            if (lane < count) {
+                const int tl = tile0 + lane, per = a.cache.page_shift - 4;
+                int page = a.table[(int64_t)b * a.ldt + (tl >> per)];
+                if (page < 0 || page >= a.cache.num_pages) { report(a.status, PTQ_ERR_INVALID_ARG, b, 2); page = 0; }
+                bulk_load(ring_w + stage * F::chunk_bytes + lane * kTileBytes, c4_tile<HD>(a.cache, page, head, tl & ((1 << per) - 1)), kTileBytes, bar);
+            }
+            ++uses;
+        };
+        int next = c_first + warp;
+#pragma unroll
+        for (int s = 0; s < kFewStages; ++s)
+            if (next < c_last) { ask(next); next += kFewWarps; }
+        bool ok = true;
+        for (int c = c_first + warp; c < c_last; c += kFewWarps) {
+            const int stage = done % kFewStages;
+            ok = __all_sync(0xffffffffu, mbar_wait_bounded(bar_w + 8 * stage, (done / kFewStages) & 1, &abort_word));
+            if (!ok) break;
+            ++done;
+            const unsigned char* data = ring_p + stage * F::chunk_bytes;
+            const int j0 = c * F::chunk;
+            const bool whole = j0 >= lo_all && j0 + F::chunk <= hi_all;
+            float x[NT][F::tiles][4];
+#pragma unroll
+            for (int tl = 0; tl < F::tiles; ++tl) {
+                const unsigned char* side = data + tl * kTileBytes;
+                alignas(16) uint32_t kw[2][kWords];
+                C4Factors f[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int token = n8 + 8 * h;
+                    if constexpr (HD == 128) *reinterpret_cast<uint4*>(kw[h]) = *reinterpret_cast<const uint4*>(side + token * (HD / 2) + t * 16);
+                    else *reinterpret_cast<uint2*>(kw[h]) = *reinterpret_cast<const uint2*>(side + token * (HD / 2) + t * 8);
+                    const uint32_t g = *reinterpret_cast<const uint16_t*>(side + kCodes + token * kGrids + t * 8 * kWords / kC4Group * 2);
+                    f[h] = c4_factors(g | g << 16);
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[nt][tl][e] = 0.f;
+#pragma unroll
+                for (int w = 0; w < kWords; ++w) {
+                    uint32_t k0[4], k1[4];
+                    c4_unpack4(kw[0][w], f[0], k0);
+                    c4_unpack4(kw[1][w], f[1], k1);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+                            mma_f16(x[nt][tl], k0[2 * h], k1[2 * h], k0[2 * h + 1], k1[2 * h + 1], qf[nt][2 * w + h][0], qf[nt][2 * w + h][1]);
+                }
+            }
+            // softmax: the reference m is raised only when some score lies above it
+            bool above = false;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int tl = 0; tl < F::tiles; ++tl)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float v = x[nt][tl][e] * mult[nt][e & 1];
+                        if (!whole) {
+                            const int j = j0 + tl * kC4Tile + n8 + 8 * (e >> 1);
+                            if (j < lo[nt][e & 1] || j >= hi[nt][e & 1]) v = -INFINITY;
+                        }
+                        x[nt][tl][e] = v;
+                        above |= v > m[nt][e & 1];
+                    }
+            if (__any_sync(0xffffffffu, above)) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        float top = m[nt][h];
+#pragma unroll
+                        for (int tl = 0; tl < F::tiles; ++tl) top = fmaxf(top, fmaxf(x[nt][tl][h], x[nt][tl][h + 2]));
+#pragma unroll
+                        for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                        const float f = m[nt][h] == top ? 1.f : exp2_approx(m[nt][h] - top);      // 0 from -infinity
+                        m[nt][h] = top;
+                        l[nt][h] *= f;
+#pragma unroll
+                        for (int j = 0; j < kTiles; ++j) { o[nt][j][h] *= f; o[nt][j][h + 2] *= f; }
+                    }
+            }
+            uint32_t pf[NT][F::tiles][2];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                float ref[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) ref[h] = (m[nt][h] == -INFINITY ? 0.f : m[nt][h]) - kAttnPShift;
+#pragma unroll
+                for (int tl = 0; tl < F::tiles; ++tl) {
+                    float pr[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        pr[e] = exp2_approx(x[nt][tl][e] - ref[e & 1]);
+                        l[nt][e & 1] += pr[e];
+                    }
+                    pf[nt][tl][0] = transpose8(pack_half2(pr[0], pr[1]));
+                    pf[nt][tl][1] = transpose8(pack_half2(pr[2], pr[3]));
+                }
+            }
+#pragma unroll
+            for (int tl = 0; tl < F::tiles; ++tl) {
+                const unsigned char* side = data + tl * kTileBytes + kSide;
+                constexpr int kV = HD / 64;                       // words a lane: 16 or 8 values of a token
+                alignas(8) uint32_t vw[4][kV];
+                uint32_t g[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int token = 2 * t + (e & 1) + 8 * (e >> 1);
+                    if constexpr (HD == 128) *reinterpret_cast<uint2*>(vw[e]) = *reinterpret_cast<const uint2*>(side + token * (HD / 2) + n8 * 8);
+                    else vw[e][0] = *reinterpret_cast<const uint32_t*>(side + token * (HD / 2) + n8 * 4);
+                    g[e] = *reinterpret_cast<const uint16_t*>(side + kCodes + token * kGrids + n8 * 8 * kV / kC4Group * 2);
+                    if (!whole) {                                 // what nobody sees may hold anything: 0 times it has to be 0
+                        const int j = j0 + tl * kC4Tile + token;
+                        if (j < lo_any || j >= hi_any) g[e] = 0u;
+                    }
+                }
+                const C4Factors f0 = c4_factors(g[0] | g[1] << 16), f1 = c4_factors(g[2] | g[3] << 16);
+#pragma unroll
+                for (int w = 0; w < kV; ++w)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t v0[4], v1[4];
+                        c4_unpack4(__byte_perm(vw[0][w], vw[1][w], h ? 0x7632 : 0x5410), f0, v0);
+                        c4_unpack4(__byte_perm(vw[2][w], vw[3][w], h ? 0x7632 : 0x5410), f1, v1);
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt)
+                                mma_f16(o[nt][4 * w + 2 * h + e], v0[2 * e], v0[2 * e + 1], v1[2 * e], v1[2 * e + 1], pf[nt][tl][0], pf[nt][tl][1]);
+                    }
+            }
+            __syncwarp();                                         // the stage has been read
+            if (next < c_last) { ask(next); next += kFewWarps; }
+        }
+        if (!ok) {                                                // copies in flight land before the ring is reused or left
+            for (; done < uses; ++done) drain_copy(bar_w + 8 * (done % kFewStages), (done / kFewStages) & 1);
+            if (lane == 0) report(a.status, PTQ_ERR_TIMEOUT, blockIdx.x, 3);
+        }
+
+        // the warps' results become one, through the ring: [warp][row][value]
+        __syncthreads();
+        float* joint = reinterpret_cast<float*>(ring);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) l[nt][h] += __shfl_xor_sync(0xffffffffu, l[nt][h], d);
+                const int row = nt * 8 + 2 * t + h;
+                if (n8 == 0) { stat_m[warp][row] = m[nt][h]; stat_l[warp][row] = l[nt][h]; }
+                float* dst = joint + (warp * kRows + row) * HD + n8 * (HD / 8);
+#pragma unroll
+                for (int j = 0; j < kTiles; ++j) *reinterpret_cast<float2*>(dst + 2 * j) = make_float2(o[nt][j][h], o[nt][j][h + 2]);
+            }
+        __syncthreads();
+        const bool complete = from == 0 && to == r.chunks;
+        float* slot = a.partial + (int64_t)(2 * blockIdx.x + (from == 0 ? 1 : 0)) * few_partial_floats(HD, NT);
+        for (int e = threadIdx.x; e < live_rows * (HD / 2); e += kFewThreads) {
+            const int row = e / (HD / 2), d = e % (HD / 2) * 2;
+            float top = -INFINITY, sum = 0.f, v0 = 0.f, v1 = 0.f;
+#pragma unroll
+            for (int w = 0; w < kFewWarps; ++w) top = fmaxf(top, stat_m[w][row]);
+            const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+            for (int w = 0; w < kFewWarps; ++w) {
+                const float f = exp2_approx(stat_m[w][row] - ref);
+                const float2 v = *reinterpret_cast<const float2*>(joint + (w * kRows + row) * HD + d);
+                sum += f * stat_l[w][row];
+                v0 += f * v.x;
+                v1 += f * v.y;
+            }
+            if (complete) {
+                const int rr = first_row + row, i = rr / a.ratio, qh = head * a.ratio + rr - i * a.ratio;
+                const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                T* out = static_cast<T*>(a.out) + (int64_t)(r.row0 + i) * a.o_token + (int64_t)qh * a.o_head + d;
+                out[0] = from_f32<T>(v0 * inv);
+                out[1] = from_f32<T>(v1 * inv);
+                if (d == 0 && a.lse) a.lse[(int64_t)(r.row0 + i) * a.q_heads + qh] = sum == 0.f ? -INFINITY : (ref + log2f(sum) - kAttnPShift) * 0.693147180559945309f;
+            } else {
+                *reinterpret_cast<float2*>(slot + row * HD + d) = make_float2(v0, v1);
+                if (d == 0) { slot[kRows * HD + row] = top; slot[kRows * (HD + 1) + row] = sum; }
+            }
+        }
+        __syncthreads();
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the ring is written by copies again
+        if (abort_word) return;
+    }
+}
+
+// Joins the partial results of what several CTAs share: one warp a row.
+template <typename T, int HD, int NT>
+__global__ void __launch_bounds__(kFewThreads) attn4_join_kernel(Attn4 a, int ctas) {
+    using F = FewShape<HD>;
+    constexpr int kRows = 8 * NT, kLane = HD / 32;
+    __shared__ FewScan scan;
+    __shared__ long long starts[kFewThreads];
+    chained_begin();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const long long total = few_total<kRows, F::chunk>(a, scan), share = few_share(total, ctas);
+    if (share >= total) return;                                   // one CTA had everything
+    const int64_t rh = (int64_t)blockIdx.x * kFewWarps + warp;
+    const int token = (int)(rh / a.q_heads), qh = (int)(rh - (int64_t)token * a.q_heads);
+    int b = -1;
+    long long before = 0;
+    for (long long base = 0, first = 0; first < a.batch; first += kFewThreads) {
+        const int mine_b = (int)first + threadIdx.x;
+        const long long mine = mine_b < a.batch ? attn_request<kRows, F::chunk>(a, mine_b).units : 0;
+        long long all;
+        starts[threadIdx.x] = base + few_scan(mine, scan, all);
+        __syncthreads();
+        for (int i = lane; i < kFewThreads && first + i < a.batch; i += 32)
+            if (a.cu[first + i] <= token && token < a.cu[first + i + 1]) { b = (int)first + i; before = starts[i]; }
+        base += all;
+        __syncthreads();
+    }
+    const unsigned has = __ballot_sync(0xffffffffu, b >= 0);
+    if (token >= a.total_q || !has) return;
+    const int src = __ffs(has) - 1;
+    b = __shfl_sync(0xffffffffu, b, src);
+    before = __shfl_sync(0xffffffffu, before, src);
+    const AttnRequest r = attn_request<kRows, F::chunk>(a, b);
+    if (r.units == 0 || token < r.row0 || token >= r.row0 + r.n) return;
+    const int head = qh / a.ratio, row = (token - r.row0) * a.ratio + qh - head * a.ratio, tile = row / kRows, in = row - tile * kRows;
+    const long long s0 = before + ((long long)head * r.tiles + tile) * r.chunks, s1 = s0 + r.chunks - 1;
+    const int c0 = (int)(s0 / share), c1 = (int)(s1 / share);
+    if (c0 == c1) return;                                         // written whole
+    float top = -INFINITY, sum = 0.f, v[kLane];
+#pragma unroll
+    for (int i = 0; i < kLane; ++i) v[i] = 0.f;
+    for (int c = c0; c <= c1; ++c) top = fmaxf(top, a.partial[(int64_t)(2 * c + (c == c0)) * few_partial_floats(HD, NT) + kRows * HD + in]);
+    const float ref = top == -INFINITY ? 0.f : top;
+    for (int c = c0; c <= c1; ++c) {
+        const float* slot = a.partial + (int64_t)(2 * c + (c == c0)) * few_partial_floats(HD, NT);
+        const float f = exp2_approx(slot[kRows * HD + in] - ref);
+        sum += f * slot[kRows * (HD + 1) + in];
+#pragma unroll
+        for (int i = 0; i < kLane; ++i) v[i] += f * slot[in * HD + lane * kLane + i];
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    T* out = static_cast<T*>(a.out) + (int64_t)token * a.o_token + (int64_t)qh * a.o_head + lane * kLane;
+#pragma unroll
+    for (int i = 0; i < kLane; ++i) out[i] = from_f32<T>(v[i] * inv);
+    if (lane == 0 && a.lse) a.lse[(int64_t)token * a.q_heads + qh] = sum == 0.f ? -INFINITY : (ref + log2f(sum) - kAttnPShift) * 0.693147180559945309f;
+}
+
+}  // namespace ptq

@@ -128,6 +128,21 @@ inline void launch_chained(void (*kernel)(Params...), dim3 grid, dim3 block, siz
     cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);       // an error stays for launch_status()
 }
 
+// The same as clusters of `cluster` CTAs along x.
+template <typename... Params, typename... Args>
+inline void launch_chained_cluster(void (*kernel)(Params...), dim3 grid, int cluster, dim3 block, size_t smem, cudaStream_t stream,
+                                   Args... args) {
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.gridDim = grid; cfg.blockDim = block; cfg.dynamicSmemBytes = smem; cfg.stream = stream;
+    cfg.attrs = attr; cfg.numAttrs = 2;
+    cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
+}
+
 inline int launch_status() { return cudaGetLastError() == cudaSuccess ? PTQ_OK : PTQ_ERR_CUDA; }
 
 inline int cdiv(int a, int b) { return (a + b - 1) / b; }
@@ -141,7 +156,8 @@ constexpr long long kSpinLimitCycles = 4000000000LL;
 // (cudaFuncSetAttribute is per device).  One table, one mutex; looked up with the caller's device current.
 // ---------------------------------------------------------------------------------------------------------
 constexpr int kMaxDevices = 64;
-enum SmemAttrSlot { SA_CHOL = 0, SA_SWEEP, SA_GRAM, SA_DGEMM, SA_SMALL, SA_XGEMM, SA_FACTOR_SWEEP, SA_GATHER, SA_COUNT };
+enum SmemAttrSlot { SA_CHOL = 0, SA_SWEEP, SA_GRAM, SA_DGEMM, SA_SMALL, SA_XGEMM, SA_FACTOR_SWEEP, SA_GATHER, SA_F8_PRODUCT, SA_CACHE_ATTN,
+                    SA_COUNT };
 struct DeviceState {
     int sms = 0;
     int coop = 0;
@@ -192,7 +208,9 @@ enum KernelId {
     K_DGEMM_LAUUM, K_MINMAX_GRID, K_SCORE_PARTIAL,
     K_SCORE_FINAL, K_RANK_SORT, K_PERM_CHECK, K_SWEEP_GATHER, K_SWEEP_COOP, K_FINALIZE,
     K_DGEMM_LOSS, K_SUM_PARTIALS, K_SELFTEST, K_FP64_PROBE, K_DYN_AUX, K_DYN_GATHER,
-    K_DGEMM_DYN, K_PER_ROW, K_DGEMM_EQ11, K_X_SLICE, K_X_GEMM, K_FACTOR_SWEEP, K_COUNT
+    K_DGEMM_DYN, K_PER_ROW, K_DGEMM_EQ11, K_X_SLICE, K_X_GEMM, K_FACTOR_SWEEP,
+    K_F8_QUANTIZE, K_F8_PRODUCT, K_F8_PRODUCT_FEW, K_CACHE_PLAN, K_CACHE_APPEND, K_CACHE_READ, K_CACHE_ATTN_FEW, K_CACHE_ATTN_JOIN,
+    K_COUNT
 };
 
 inline const char* kernel_name(int id) {
@@ -201,7 +219,9 @@ inline const char* kernel_name(int id) {
         "dgemm_lauum",
         "minmax_grid", "score_partial", "score_final", "rank_sort", "perm_check", "sweep_gather",
         "sweep_coop", "finalize", "dgemm_loss", "sum_partials", "selftest", "fp64_probe", "dyn_aux", "dyn_gather",
-        "dgemm_dyn", "per_row", "dgemm_eq11", "x_slice", "i8gemm_tcgen05", "factor_sweep"};
+        "dgemm_dyn", "per_row", "dgemm_eq11", "x_slice", "i8gemm_tcgen05", "factor_sweep",
+        "f8_quantize", "f8_product_tcgen05", "f8_product_few_tcgen05", "cache_plan", "cache_append", "cache_read", "cache_attn_few",
+        "cache_attn_join"};
     return (id >= 0 && id < K_COUNT) ? names[id] : "unknown";
 }
 

@@ -1,0 +1,300 @@
+// C-ABI entry points of the low-bit serving operators (see include/ptq.h): argument checks and the choice of kernels.
+#include "cache4.cuh"
+#include "common.cuh"
+#include "fp8.cuh"
+
+using namespace ptq;
+
+namespace {
+
+int type_size(int type) { return type == PTQ_F32 ? 4 : type == PTQ_F16 || type == PTQ_BF16 ? 2 : 0; }
+
+// Calls f with a null pointer of the type that `type` names.
+template <typename F>
+int with_type(int type, F f) {
+    switch (type) {
+        case PTQ_F32: return f(static_cast<float*>(nullptr));
+        case PTQ_F16: return f(static_cast<__half*>(nullptr));
+        case PTQ_BF16: return f(static_cast<__nv_bfloat16*>(nullptr));
+    }
+    return PTQ_ERR_INVALID_ARG;
+}
+
+int page_shift_of(int page_size) {
+    for (int s = 4; s <= 10; ++s)
+        if (page_size == 1 << s) return s;
+    return -1;
+}
+
+template <typename T, int NT>
+cudaError_t allow_few_smem() {
+    return cudaFuncSetAttribute(f8_product_few_kernel<T, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, F8Few<NT>::smem_bytes);
+}
+template <typename T>
+cudaError_t allow_f8_smem() {
+    cudaError_t e = cudaFuncSetAttribute(f8_product_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kF8SmemBytes);
+    if (e == cudaSuccess) e = allow_few_smem<T, 16>();
+    if (e == cudaSuccess) e = allow_few_smem<T, 32>();
+    if (e == cudaSuccess) e = allow_few_smem<T, 64>();
+    if (e == cudaSuccess) e = allow_few_smem<T, 128>();
+    return e;
+}
+
+template <typename T, int NT>
+int f8_few_launch(const F8Product& p, const uint8_t* A, int64_t lda, const uint8_t* B, int64_t ldb, int ks, cudaStream_t stream) {
+    CUtensorMap mapA, mapB;
+    int st = f8_map(&mapA, A, p.m, p.k, lda, NT);
+    if (!st) st = f8_map(&mapB, B, p.n, p.k, ldb, 128);
+    if (st) return st;
+    Launch l(K_F8_PRODUCT_FEW, stream);
+    launch_chained_cluster(f8_product_few_kernel<T, NT>, dim3(ks, cdiv(p.n, 128), cdiv(p.m, NT)), ks, kF8FewThreads,
+                           F8Few<NT>::smem_bytes, stream, mapA, mapB, p, ks);
+    return PTQ_OK;
+}
+
+template <typename T>
+int f8_launch(const F8Product& p, const uint8_t* A, int64_t lda, const uint8_t* B, int64_t ldb, int sms, cudaStream_t stream) {
+    const long tiles_m = cdiv(p.m, kF8TileM), tiles_n = cdiv(p.n, kF8TileN);
+    if (tiles_m * tiles_n >= sms) {
+        CUtensorMap mapA, mapB;
+        int st = f8_map(&mapA, A, p.m, p.k, lda, kF8TileM);
+        if (!st) st = f8_map(&mapB, B, p.n, p.k, ldb, kF8TileN);
+        if (st) return st;
+        const int grid = (int)(tiles_m * tiles_n < sms ? tiles_m * tiles_n : sms);
+        Launch l(K_F8_PRODUCT, stream);
+        launch_chained(f8_product_kernel<T>, grid, kF8Threads, kF8SmemBytes, stream, mapA, mapB, p, (int)tiles_m, (int)tiles_n);
+        return PTQ_OK;
+    }
+    const int nt = p.m <= 16 ? 16 : p.m <= 32 ? 32 : p.m <= 64 ? 64 : 128;
+    const long tiles = (long)cdiv(p.n, 128) * cdiv(p.m, nt);
+    int ks = 1;
+    while (ks < 8 && tiles * ks * 2 <= 2 * sms && ks * 2 <= p.kb) ks *= 2;
+    switch (nt) {
+        case 16: return f8_few_launch<T, 16>(p, A, lda, B, ldb, ks, stream);
+        case 32: return f8_few_launch<T, 32>(p, A, lda, B, ldb, ks, stream);
+        case 64: return f8_few_launch<T, 64>(p, A, lda, B, ldb, ks, stream);
+    }
+    return f8_few_launch<T, 128>(p, A, lda, B, ldb, ks, stream);
+}
+
+int cache_check(Cache4* c, const void* pages, int num_pages, int page_size, int kv_heads, int head_dim) {
+    const int shift = page_shift_of(page_size);
+    if (!pages || num_pages < 1 || kv_heads < 1 || head_dim < 1) return PTQ_ERR_INVALID_ARG;
+    if (shift < 0 || (head_dim != 64 && head_dim != 128) || kv_heads > 65535) return PTQ_ERR_UNSUPPORTED;
+    if ((int64_t)num_pages * page_size > 0x7fffffffll) return PTQ_ERR_UNSUPPORTED;       // slots are int32
+    if (!aligned16(pages)) return PTQ_ERR_ALIGNMENT;
+    c->pages = static_cast<uint8_t*>(const_cast<void*>(pages));
+    c->num_pages = num_pages;
+    c->page_shift = shift;
+    c->kv_heads = kv_heads;
+    return PTQ_OK;
+}
+
+bool rows_aligned(const void* p, int64_t a, int64_t b, int size) { return aligned16(p) && a * size % 16 == 0 && b * size % 16 == 0; }
+
+// Append and read share their arguments.
+int cache_tokens(bool append, const Cache4& c, int head_dim, C4Tokens a, int type, cudaStream_t stream) {
+    a.vec = rows_aligned(a.k, a.k_token, a.k_head, type_size(type)) && rows_aligned(a.v, a.v_token, a.v_head, type_size(type));
+    const int64_t threads = (int64_t)a.tokens * c.kv_heads * 2 * (head_dim / 8), grid = (threads + 255) / 256;
+    if (grid > 0x7fffffffll) return PTQ_ERR_UNSUPPORTED;
+    return with_type(type, [&](auto* t) {
+        using T = std::remove_pointer_t<decltype(t)>;
+        Launch l(append ? K_CACHE_APPEND : K_CACHE_READ, stream);
+        if (append) {
+            if (head_dim == 128) launch_chained(cache_append_kernel<T, 128>, (unsigned)grid, 256, 0, stream, c, a);
+            else launch_chained(cache_append_kernel<T, 64>, (unsigned)grid, 256, 0, stream, c, a);
+        } else {
+            if (head_dim == 128) launch_chained(cache_read_kernel<T, 128>, (unsigned)grid, 256, 0, stream, c, a);
+            else launch_chained(cache_read_kernel<T, 64>, (unsigned)grid, 256, 0, stream, c, a);
+        }
+        return launch_status();
+    });
+}
+
+template <typename T, int HD, int NT>
+cudaError_t allow_attn_smem() {
+    return cudaFuncSetAttribute(attn4_few_kernel<T, HD, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewShape<HD>::smem_bytes);
+}
+template <typename T>
+cudaError_t allow_attn_smem_all() {
+    cudaError_t e = allow_attn_smem<T, 64, 1>();
+    if (e == cudaSuccess) e = allow_attn_smem<T, 64, 2>();
+    if (e == cudaSuccess) e = allow_attn_smem<T, 128, 1>();
+    if (e == cudaSuccess) e = allow_attn_smem<T, 128, 2>();
+    return e;
+}
+
+template <typename T, int HD, int NT>
+int attn_few_launch(const Attn4& a, int sms, cudaStream_t stream) {
+    const int want = sms * (NT == 1 ? 2 : 1), ctas = want < kFewMaxCtas ? want : kFewMaxCtas;
+    {
+        Launch l(K_CACHE_ATTN_FEW, stream);
+        launch_chained(attn4_few_kernel<T, HD, NT>, ctas, kFewThreads, FewShape<HD>::smem_bytes, stream, a);
+    }
+    {
+        Launch l(K_CACHE_ATTN_JOIN, stream);
+        launch_chained(attn4_join_kernel<T, HD, NT>, (unsigned)(((int64_t)a.total_q * a.q_heads + kFewWarps - 1) / kFewWarps),
+                       kFewThreads, 0, stream, a, ctas);
+    }
+    return launch_status();
+}
+
+// Rows of one request and kv head that the kernel for few rows takes at once.
+int few_tiles(int64_t rows) { return rows <= 8 ? 1 : 2; }
+
+}  // namespace
+
+extern "C" {
+
+int ptq_fp8_quantize(const void* x, int x_type, int rows, int cols, int64_t ldx, int block_rows, uint8_t* q, int64_t ldq, float* scale,
+                     int64_t ld_scale, int32_t* status, void* stream_) {
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    const int size = type_size(x_type), kb = cols > 0 ? cdiv(cols, kF8Block) : 0;
+    if (rows < 0 || cols < 1 || !size || (block_rows != 1 && block_rows != kF8Block)) return PTQ_ERR_INVALID_ARG;
+    if (rows == 0) return PTQ_OK;
+    if (!x || !q || !scale || ldx < cols || ldq < cols || ld_scale < kb) return PTQ_ERR_INVALID_ARG;
+    if (cols > 0x7fffff00 || (block_rows > 1 && cdiv(rows, kF8Block) > 65535)) return PTQ_ERR_UNSUPPORTED;
+    if (!aligned16(q) || ldq % 16) return PTQ_ERR_ALIGNMENT;
+    const int vec = aligned16(x) && ldx * size % 16 == 0;
+    return with_type(x_type, [&](auto* t) {
+        using T = std::remove_pointer_t<decltype(t)>;
+        const T* xs = static_cast<const T*>(x);
+        if (block_rows == 1) {
+            const int64_t grid = ((int64_t)rows * kb + 16 * kF8RowUnroll - 1) / (16 * kF8RowUnroll);
+            if (grid > 0x7fffffffll) return (int)PTQ_ERR_UNSUPPORTED;
+            Launch l(K_F8_QUANTIZE, stream);
+            launch_chained(f8_quantize_rows_kernel<T>, (unsigned)grid, 256, 0, stream, xs, rows, cols, ldx, vec, q, ldq, scale, ld_scale,
+                           status);
+        } else {
+            Launch l(K_F8_QUANTIZE, stream);
+            launch_chained(f8_quantize_blocks_kernel<T>, dim3(kb, cdiv(rows, kF8Block)), 256, 0, stream, xs, rows, cols, ldx, vec, q, ldq,
+                           scale, ld_scale, status);
+        }
+        return launch_status();
+    });
+}
+
+int ptq_fp8_matmul(void* C, int c_type, int64_t ldc, const uint8_t* A, int64_t lda, const float* scale_a, int64_t ld_scale_a,
+                   const uint8_t* B, int64_t ldb, const float* scale_b, int64_t ld_scale_b, int m, int n, int k, int32_t* status,
+                   void* stream_) {
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    const int kb = k > 0 ? cdiv(k, kF8Block) : 0;
+    if (m < 0 || n < 0 || k < 1 || !type_size(c_type)) return PTQ_ERR_INVALID_ARG;
+    if (m == 0 || n == 0) return PTQ_OK;
+    if (!C || !A || !B || !scale_a || !scale_b || ldc < n || lda < k || ldb < k || ld_scale_a < kb || ld_scale_b < kb)
+        return PTQ_ERR_INVALID_ARG;
+    if (k > 0x7fffff00 || (int64_t)cdiv(m, 16) > 65535 || (int64_t)cdiv(n, 128) > 65535) return PTQ_ERR_UNSUPPORTED;
+    if (!aligned16(A) || !aligned16(B) || lda % 16 || ldb % 16) return PTQ_ERR_ALIGNMENT;
+    DeviceState* dev = nullptr;
+    int st = current_device_state(&dev);
+    if (st) return st;
+    st = ensure_smem_attr(dev, SA_F8_PRODUCT, [] {
+        cudaError_t e = allow_f8_smem<float>();
+        if (e == cudaSuccess) e = allow_f8_smem<__half>();
+        if (e == cudaSuccess) e = allow_f8_smem<__nv_bfloat16>();
+        return e;
+    });
+    if (st) return st;
+    F8Product p{C, scale_a, scale_b, ldc, ld_scale_a, ld_scale_b, m, n, k, kb, status};
+    st = with_type(c_type, [&](auto* t) { return f8_launch<std::remove_pointer_t<decltype(t)>>(p, A, lda, B, ldb, dev->sms, stream); });
+    return st ? st : launch_status();
+}
+
+size_t ptq_cache_page_bytes(int page_size, int kv_heads, int head_dim) {
+    if (page_shift_of(page_size) < 0 || kv_heads < 1 || kv_heads > 65535 || (head_dim != 64 && head_dim != 128)) return 0;
+    return (size_t)kv_heads * (page_size / kC4Tile) * c4_tile_bytes(head_dim);
+}
+
+int ptq_cache_plan(const int32_t* kv_lens, const int32_t* new_tokens, int batch, int page_size, int32_t* block_table, int64_t ld_table,
+                   int max_pages, const int32_t* free_pages, int num_free, int32_t* slots, int32_t* positions, int max_tokens,
+                   int32_t* cu_q, int32_t* kv_lens_out, int32_t* taken, int32_t* status, void* stream_) {
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    const int shift = page_shift_of(page_size);
+    if (batch < 0 || max_pages < 0 || ld_table < max_pages || num_free < 0 || max_tokens < 0 || !cu_q || !taken) return PTQ_ERR_INVALID_ARG;
+    if (batch > 0 && (!kv_lens || !new_tokens || !kv_lens_out || (max_pages > 0 && !block_table))) return PTQ_ERR_INVALID_ARG;
+    if ((num_free > 0 && !free_pages) || (max_tokens > 0 && (!slots || !positions))) return PTQ_ERR_INVALID_ARG;
+    if (batch > 0 && kv_lens_out < kv_lens + batch && kv_lens < kv_lens_out + batch) return PTQ_ERR_INVALID_ARG;     // read by every CTA
+    if (shift < 0 || (int64_t)max_pages * page_size > 0x7fffffffll) return PTQ_ERR_UNSUPPORTED;
+    CachePlan p{kv_lens, new_tokens, batch, block_table, ld_table, max_pages, free_pages, num_free, shift, slots, positions, max_tokens,
+                cu_q, kv_lens_out, taken, status};
+    const int grid = max_tokens > kPlanTokens ? (int)(((int64_t)max_tokens + kPlanTokens - 1) / kPlanTokens) : 1;
+    Launch l(K_CACHE_PLAN, stream);
+    launch_chained(cache_plan_kernel, grid, kPlanThreads, 0, stream, p);
+    return launch_status();
+}
+
+int ptq_cache_append(void* pages, int num_pages, int page_size, int kv_heads, int head_dim, const void* k, int64_t k_token, int64_t k_head,
+                     const void* v, int64_t v_token, int64_t v_head, int type, const int32_t* slots, int tokens, int32_t* status,
+                     void* stream_) {
+    Cache4 c;
+    const int st = cache_check(&c, pages, num_pages, page_size, kv_heads, head_dim);
+    if (st) return st;
+    if (tokens < 0 || !type_size(type)) return PTQ_ERR_INVALID_ARG;
+    if (tokens == 0) return PTQ_OK;
+    if (!k || !v || !slots || k_token < 0 || k_head < 0 || v_token < 0 || v_head < 0) return PTQ_ERR_INVALID_ARG;
+    return cache_tokens(true, c, head_dim,
+                        C4Tokens{const_cast<void*>(k), const_cast<void*>(v), k_token, k_head, v_token, v_head, slots, tokens, 0, status},
+                        type, static_cast<cudaStream_t>(stream_));
+}
+
+int ptq_cache_read(const void* pages, int num_pages, int page_size, int kv_heads, int head_dim, void* k, int64_t k_token, int64_t k_head,
+                   void* v, int64_t v_token, int64_t v_head, int type, const int32_t* slots, int tokens, int32_t* status, void* stream_) {
+    Cache4 c;
+    const int st = cache_check(&c, pages, num_pages, page_size, kv_heads, head_dim);
+    if (st) return st;
+    if (tokens < 0 || !type_size(type)) return PTQ_ERR_INVALID_ARG;
+    if (tokens == 0) return PTQ_OK;
+    if (!k || !v || !slots || k_token < head_dim || k_head < head_dim || v_token < head_dim || v_head < head_dim) return PTQ_ERR_INVALID_ARG;
+    return cache_tokens(false, c, head_dim, C4Tokens{k, v, k_token, k_head, v_token, v_head, slots, tokens, 0, status}, type,
+                        static_cast<cudaStream_t>(stream_));
+}
+
+size_t ptq_cache_attention_workspace_bytes(int q_heads, int kv_heads, int head_dim, int max_q) {
+    if (q_heads < 1 || kv_heads < 1 || q_heads % kv_heads || max_q < 1 || (head_dim != 64 && head_dim != 128)) return 0;
+    const int nt = few_tiles((int64_t)max_q * (q_heads / kv_heads));
+    return align_up((size_t)2 * kFewMaxCtas * few_partial_floats(head_dim, nt) * sizeof(float));
+}
+
+int ptq_cache_attention(void* out, int64_t o_token, int64_t o_head, float* lse, const void* q, int64_t q_token, int64_t q_head, int type,
+                        int q_heads, const void* pages, int num_pages, int page_size, int kv_heads, int head_dim,
+                        const int32_t* block_table, int64_t ld_table, int max_pages, const int32_t* kv_lens, const int32_t* cu_q,
+                        int batch, int total_q, int max_q, float scale, int causal, int window, void* ws, size_t ws_bytes,
+                        int32_t* status, void* stream_) {
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    Attn4 a{};
+    int st = cache_check(&a.cache, pages, num_pages, page_size, kv_heads, head_dim);
+    if (st) return st;
+    if (q_heads < 1 || q_heads % kv_heads || batch < 0 || total_q < 0 || max_q < 0 || max_pages < 0 || ld_table < max_pages || window < 0 ||
+        (causal != 0 && causal != 1) || (type != PTQ_F16 && type != PTQ_BF16) || !(scale - scale == 0.f))
+        return PTQ_ERR_INVALID_ARG;
+    if (batch == 0 || total_q == 0 || max_q == 0) return PTQ_OK;
+    if (!out || !q || !kv_lens || !cu_q || (max_pages > 0 && !block_table) || o_token < head_dim || o_head < head_dim || q_token < 0 || q_head < 0)
+        return PTQ_ERR_INVALID_ARG;
+    if ((int64_t)max_pages * page_size > 0x7fffffffll || (int64_t)total_q * q_heads > 0x7fffffffll) return PTQ_ERR_UNSUPPORTED;
+    if (!aligned16(ws)) return PTQ_ERR_ALIGNMENT;
+    if (!ws || ws_bytes < ptq_cache_attention_workspace_bytes(q_heads, kv_heads, head_dim, max_q)) return PTQ_ERR_WORKSPACE;
+    DeviceState* dev = nullptr;
+    st = current_device_state(&dev);
+    if (st) return st;
+    st = ensure_smem_attr(dev, SA_CACHE_ATTN, [] {
+        const cudaError_t e = allow_attn_smem_all<__half>();
+        return e == cudaSuccess ? allow_attn_smem_all<__nv_bfloat16>() : e;
+    });
+    if (st) return st;
+    a.q = q; a.out = out; a.lse = lse;
+    a.q_token = q_token; a.q_head = q_head; a.o_token = o_token; a.o_head = o_head;
+    a.table = block_table; a.ldt = ld_table; a.max_pages = max_pages; a.lens = kv_lens; a.cu = cu_q;
+    a.batch = batch; a.total_q = total_q; a.q_heads = q_heads; a.ratio = q_heads / kv_heads;
+    a.scale_log2 = scale * 1.4426950408889634f;
+    a.causal = causal; a.window = window; a.row_limit = 0x7fffffff;
+    a.partial = static_cast<float*>(ws); a.status = status;
+    const int nt = few_tiles((int64_t)max_q * a.ratio);
+    auto launch = [&](auto* t) {
+        using T = std::remove_pointer_t<decltype(t)>;
+        if (head_dim == 64) return nt == 1 ? attn_few_launch<T, 64, 1>(a, dev->sms, stream) : attn_few_launch<T, 64, 2>(a, dev->sms, stream);
+        return nt == 1 ? attn_few_launch<T, 128, 1>(a, dev->sms, stream) : attn_few_launch<T, 128, 2>(a, dev->sms, stream);
+    };
+    return type == PTQ_F16 ? launch(static_cast<__half*>(nullptr)) : launch(static_cast<__nv_bfloat16*>(nullptr));
+}
+
+}  // extern "C"

@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import c_double, c_int, c_int64, c_size_t, c_void_p
+from ctypes import c_double, c_float, c_int, c_int64, c_size_t, c_void_p
 
 import torch
 
@@ -31,7 +31,13 @@ EXPORTS = ["ptq_workspace_bytes", "ptq_hessian_accumulate", "ptq_hessian_accumul
            "ptq_sort_scores", "ptq_gemm_nt_sliced", "ptq_gemm_nt_sliced_workspace_bytes", "ptq_quantize_layer_dynamic", "ptq_quantize_layer_per_row", "ptq_selftest_wait_timeout", "ptq_selftest_abandoned_sweep",
            "ptq_selftest_reciprocal", "ptq_fp64_probe",
            "ptq_kernel_count", "ptq_kernel_name", "ptq_launch_count", "ptq_profile_enable", "ptq_profile_read",
-           "ptq_set_cta_limit"]
+           "ptq_set_cta_limit",
+           "ptq_fp8_quantize", "ptq_fp8_matmul", "ptq_cache_page_bytes", "ptq_cache_plan", "ptq_cache_append", "ptq_cache_read",
+           "ptq_cache_attention", "ptq_cache_attention_workspace_bytes"]
+
+F32, F16, BF16 = range(3)
+FP8_BLOCK = 128               # values under one scale of an 8-bit operand
+CACHE_TILE = 16               # tokens of one tile of the 4-bit cache
 
 
 class PtqError(RuntimeError):
@@ -78,6 +84,20 @@ def lib():
                                                  vp, c_size_t, vp, vp]
         L.ptq_quantize_layer_dynamic.argtypes = [vp, c_int, c_int, c_int64, vp, vp, vp, c_int, c_int, c_int, vp, vp,
                                                  vp, vp, vp, vp, c_size_t, vp, vp]
+        L.ptq_fp8_quantize.argtypes = [vp, c_int, c_int, c_int, c_int64, c_int, vp, c_int64, vp, c_int64, vp, vp]
+        L.ptq_fp8_matmul.argtypes = [vp, c_int, c_int64, vp, c_int64, vp, c_int64, vp, c_int64, vp, c_int64, c_int, c_int, c_int,
+                                     vp, vp]
+        L.ptq_cache_page_bytes.argtypes = [c_int, c_int, c_int]
+        L.ptq_cache_page_bytes.restype = c_size_t
+        L.ptq_cache_plan.argtypes = [vp, vp, c_int, c_int, vp, c_int64, c_int, vp, c_int, vp, vp, c_int, vp, vp, vp, vp, vp]
+        for name in ("ptq_cache_append", "ptq_cache_read"):
+            getattr(L, name).argtypes = [vp, c_int, c_int, c_int, c_int, vp, c_int64, c_int64, vp, c_int64, c_int64, c_int, vp,
+                                         c_int, vp, vp]
+        L.ptq_cache_attention_workspace_bytes.argtypes = [c_int, c_int, c_int, c_int]
+        L.ptq_cache_attention_workspace_bytes.restype = c_size_t
+        L.ptq_cache_attention.argtypes = [vp, c_int64, c_int64, vp, vp, c_int64, c_int64, c_int, c_int, vp, c_int, c_int, c_int,
+                                          c_int, vp, c_int64, c_int, vp, vp, c_int, c_int, c_int, c_float, c_int, c_int, vp,
+                                          c_size_t, vp, vp]
         L.ptq_selftest_wait_timeout.argtypes = [c_int, ctypes.c_longlong, vp, c_size_t, vp, vp]
         L.ptq_selftest_abandoned_sweep.argtypes = [ctypes.c_longlong, vp, c_size_t, vp, vp, vp]
         L.ptq_selftest_reciprocal.argtypes = [vp, c_int, vp, vp, vp]
@@ -343,6 +363,225 @@ def quantize_layer_per_row(W, Hinv, scale, zero, bits, score_mode, codes, What, 
                                             int(bits), int(score_mode), _ptr(codes), _ptr(What), _ptr(perm_rows),
                                             _ptr(H_undamped), _ptr(loss_out), _ptr(buf), buf.numel(), _ptr(status),
                                             _stream(stream)), "ptq_quantize_layer_per_row")
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# Serving a quantized network: products in 8-bit floating point and a key-value cache held in 4 bits.  Every call below runs
+# on the device of its tensors, whatever the current device is, and on that device's current stream unless one is given.
+# ---------------------------------------------------------------------------------------------------------------------
+_TYPE_IDS = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
+
+
+def _type_id(t, name, half_only=False):
+    if t.dtype not in _TYPE_IDS or (half_only and t.dtype == torch.float32):
+        raise ValueError(f"{name} must be " + ("" if half_only else "float32, ") + "float16 or bfloat16")
+    return _TYPE_IDS[t.dtype]
+
+
+def _ld(t, name):
+    """Row stride of a 2-D tensor with contiguous rows; sizes of 0 and 1 leave strides undefined."""
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1 and t.shape[0] > 0):
+        raise ValueError(f"{name} must be 2-D with unit column stride")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _strides(t, name):
+    """(token stride, head stride) of [tokens, heads, dim] with contiguous heads, in elements."""
+    tokens, heads, dim = t.shape
+    a, b, c = t.stride()
+    if c != 1 and t.numel():
+        raise ValueError(f"{name} must have unit stride within a head")
+    return a if tokens > 1 else heads * dim, b if heads > 1 else dim
+
+
+def _bytes8(t, name):
+    if t.dtype not in (torch.float8_e4m3fn, torch.uint8):
+        raise ValueError(f"{name} must be float8_e4m3fn (or uint8)")
+    return _ld(t, name)
+
+
+def _ints(name, t, shape=None):
+    _dev(t, torch.int32, name)
+    if not t.is_contiguous() or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{name} must be contiguous" + ("" if shape is None else f" {list(shape)}"))
+    return t
+
+
+def _shape(name, t, shape):
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {list(shape)}, not {list(t.shape)}")
+
+
+def _on_one_device(*tensors):
+    """The device of all these tensors (None among them is skipped)."""
+    dev = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError("tensors must be CUDA tensors (the library has no CPU path)")
+        if dev is not None and t.device != dev:
+            raise ValueError(f"tensors are on {dev} and {t.device}: they must share a device")
+        dev = t.device
+    return dev
+
+
+def _span(t):
+    """[first, last] byte that a tensor's elements touch."""
+    last = sum((n - 1) * st for n, st in zip(t.shape, t.stride())) * t.element_size()
+    return t.data_ptr(), t.data_ptr() + last + t.element_size() - 1
+
+
+def _apart(name, out, *inputs):
+    """Refuses an output that shares memory with an input."""
+    if out is None or out.numel() == 0:
+        return
+    a, b = _span(out)
+    for t in inputs:
+        if t is not None and t.numel():
+            c, d = _span(t)
+            if a <= d and c <= b:
+                raise ValueError(f"{name} must not share memory with an input")
+
+
+def _ws_for(ws, nbytes, dev):
+    buf = ws.get(nbytes)
+    if buf.device != dev:
+        raise ValueError(f"the workspace is on {buf.device}, the tensors are on {dev}")
+    return buf
+
+
+def fp8_empty(rows, cols, device="cuda"):
+    """An uninitialised float8_e4m3fn matrix [rows, cols] whose row stride is a multiple of 16 bytes, as the product wants it."""
+    return torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.float8_e4m3fn, device=device)[:, :cols]
+
+
+def fp8_quantize(x, q, scale, status, block_rows=1, stream=None):
+    """x [rows, cols] to 8-bit floating point q with a power-of-two scale for each block of block_rows x 128 values (1:
+    activations, 128: weights).  q: ``fp8_empty(rows, cols)``, scale: float32 [ceil(rows / block_rows), ceil(cols / 128)]."""
+    dev = _on_one_device(x, q, scale, status)
+    rows, cols = x.shape
+    _shape("q", q, (rows, cols))
+    _dev(scale, torch.float32, "scale")
+    _shape("scale", scale, (-(-rows // max(1, int(block_rows))), -(-cols // FP8_BLOCK)))
+    _apart("q", q, x); _apart("scale", scale, x)
+    with torch.cuda.device(dev):
+        _check(lib().ptq_fp8_quantize(_ptr(x), _type_id(x, "x"), rows, cols, _ld(x, "x"), int(block_rows), _ptr(q),
+                                      _bytes8(q, "q"), _ptr(scale), _ld(scale, "scale"), _ptr(status), _stream(stream)),
+               "ptq_fp8_quantize")
+
+
+def fp8_matmul(C, A, scale_a, B, scale_b, status, stream=None):
+    """C = A B^T for 8-bit floating-point A [m, k] with a scale per row and 128 columns and B [n, k] with one per 128 x 128, as
+    ``fp8_quantize`` makes them; C [m, n] float32, float16 or bfloat16."""
+    dev = _on_one_device(C, A, scale_a, B, scale_b, status)
+    (m, k), n = A.shape, B.shape[0]
+    _shape("B", B, (n, k)); _shape("C", C, (m, n))
+    _dev(scale_a, torch.float32, "scale_a"); _dev(scale_b, torch.float32, "scale_b")
+    kb = -(-k // FP8_BLOCK)
+    _shape("scale_a", scale_a, (m, kb)); _shape("scale_b", scale_b, (-(-n // FP8_BLOCK), kb))
+    _apart("C", C, A, scale_a, B, scale_b)
+    with torch.cuda.device(dev):
+        _check(lib().ptq_fp8_matmul(_ptr(C), _type_id(C, "C"), _ld(C, "C"), _ptr(A), _bytes8(A, "A"), _ptr(scale_a),
+                                    _ld(scale_a, "scale_a"), _ptr(B), _bytes8(B, "B"), _ptr(scale_b),
+                                    _ld(scale_b, "scale_b"), m, n, k, _ptr(status), _stream(stream)), "ptq_fp8_matmul")
+
+
+class Cache4:
+    """Pages of keys and values in 4 bits (layout: ``include/ptq.h``).  ``pages``: uint8 [num_pages, kv_heads, page_size / 16,
+    bytes of a tile], made here (uninitialised) or handed in."""
+
+    def __init__(self, num_pages, page_size, kv_heads, head_dim, device="cuda", pages=None):
+        nbytes = int(lib().ptq_cache_page_bytes(int(page_size), int(kv_heads), int(head_dim)))
+        if nbytes == 0:
+            raise PtqError(ERR_UNSUPPORTED, "Cache4")
+        shape = (num_pages, kv_heads, page_size // CACHE_TILE, nbytes // (kv_heads * (page_size // CACHE_TILE)))
+        self.num_pages, self.page_size, self.kv_heads, self.head_dim = num_pages, page_size, kv_heads, head_dim
+        if pages is None:
+            pages = torch.empty(shape, dtype=torch.uint8, device=device)
+        _dev(pages, torch.uint8, "pages"); _shape("pages", pages, shape)
+        if not pages.is_contiguous():
+            raise ValueError("pages must be contiguous")
+        self.pages = pages
+
+    def _args(self):
+        return _ptr(self.pages), self.num_pages, self.page_size, self.kv_heads, self.head_dim
+
+
+def cache_plan(kv_lens, new_tokens, block_table, free_pages, page_size, slots, positions, cu_q, kv_lens_out, taken, status,
+               stream=None):
+    """Where the new tokens of a batch go: extends ``block_table`` [batch, pages] by pages of ``free_pages``, fills ``slots`` and
+    ``positions`` [tokens] (-1 behind the last token), ``cu_q`` [batch + 1], ``kv_lens_out`` [batch] and ``taken`` [1]; all int32."""
+    dev = _on_one_device(kv_lens, new_tokens, block_table, free_pages, slots, positions, cu_q, kv_lens_out, taken, status)
+    batch, max_pages = block_table.shape
+    _dev(block_table, torch.int32, "block_table")
+    for name, t in (("kv_lens", kv_lens), ("new_tokens", new_tokens), ("kv_lens_out", kv_lens_out)):
+        _ints(name, t, (batch,))
+    _ints("cu_q", cu_q, (batch + 1,)); _ints("taken", taken, (1,)); _ints("free_pages", free_pages)
+    _ints("slots", slots); _ints("positions", positions, slots.shape)
+    outs = [("block_table", block_table), ("slots", slots), ("positions", positions), ("cu_q", cu_q), ("kv_lens_out", kv_lens_out),
+            ("taken", taken)]
+    for i, (name, t) in enumerate(outs):
+        _apart(name, t, kv_lens, new_tokens, free_pages, *[u for _, u in outs[:i]])
+    with torch.cuda.device(dev):
+        _check(lib().ptq_cache_plan(_ptr(kv_lens), _ptr(new_tokens), batch, int(page_size), _ptr(block_table),
+                                    max(_ld(block_table, "block_table"), max_pages), max_pages, _ptr(free_pages),
+                                    free_pages.numel(), _ptr(slots), _ptr(positions), slots.numel(), _ptr(cu_q),
+                                    _ptr(kv_lens_out), _ptr(taken), _ptr(status), _stream(stream)), "ptq_cache_plan")
+
+
+def _cache_tokens(fn, where, cache, k, v, slots, status, stream):
+    dev = _on_one_device(cache.pages, k, v, slots, status)
+    tokens = slots.numel()
+    _ints("slots", slots, (tokens,))
+    for name, t in (("k", k), ("v", v)):
+        _shape(name, t, (tokens, cache.kv_heads, cache.head_dim))
+    if k.dtype != v.dtype:
+        raise ValueError("k and v must have one type")
+    _apart("k", k, cache.pages, slots); _apart("v", v, cache.pages, slots)
+    with torch.cuda.device(dev):
+        _check(fn(*cache._args(), _ptr(k), *_strides(k, "k"), _ptr(v), *_strides(v, "v"), _type_id(k, "k"),
+                  _ptr(slots), tokens, _ptr(status), _stream(stream)), where)
+
+
+def cache_append(cache, k, v, slots, status, stream=None):
+    """Writes keys and values [tokens, kv_heads, head_dim] to their ``slots`` (int32, all different; negative ones are skipped)."""
+    _cache_tokens(lib().ptq_cache_append, "ptq_cache_append", cache, k, v, slots, status, stream)
+
+
+def cache_read(cache, slots, k, v, status, stream=None):
+    """The values held at ``slots`` to k and v [tokens, kv_heads, head_dim]; rows of negative slots stay as they are."""
+    _apart("k", k, v)
+    _cache_tokens(lib().ptq_cache_read, "ptq_cache_read", cache, k, v, slots, status, stream)
+
+
+def cache_attention(out, q, cache, block_table, kv_lens, cu_q, max_q, scale, ws, status, causal=True, window=0, lse=None,
+                    stream=None):
+    """Attention of the newest tokens of each request (rows cu_q[r] .. cu_q[r + 1] - 1 of q [tokens, q_heads, head_dim]) over the
+    kv_lens[r] tokens that ``cache`` holds of it.  ``max_q``: the most rows of any request.  ``window`` > 0: a row sees that many
+    keys back, itself included.  ``lse``: float32 [tokens, q_heads] for the logarithms of the sums, or None."""
+    dev = _on_one_device(out, q, cache.pages, block_table, kv_lens, cu_q, lse, status)
+    total_q, q_heads, dim = q.shape
+    batch, max_pages = block_table.shape
+    _shape("q", q, (total_q, q_heads, cache.head_dim)); _shape("out", out, q.shape)
+    if q.dtype != out.dtype:
+        raise ValueError("q and out must have one type")
+    _dev(block_table, torch.int32, "block_table")
+    _ints("kv_lens", kv_lens, (batch,)); _ints("cu_q", cu_q, (batch + 1,))
+    if lse is not None:
+        _dev(lse, torch.float32, "lse"); _shape("lse", lse, (total_q, q_heads))
+        if not lse.is_contiguous():
+            raise ValueError("lse must be contiguous")
+    _apart("out", out, q, cache.pages, block_table, kv_lens, cu_q, lse)
+    _apart("lse", lse, q, cache.pages, block_table, kv_lens, cu_q)
+    with torch.cuda.device(dev):
+        need = int(lib().ptq_cache_attention_workspace_bytes(q_heads, cache.kv_heads, dim, max(1, int(max_q))))
+        buf = _ws_for(ws, need, dev)
+        _check(lib().ptq_cache_attention(_ptr(out), *_strides(out, "out"), _ptr(lse), _ptr(q), *_strides(q, "q"),
+                                         _type_id(q, "q", half_only=True), q_heads, *cache._args(), _ptr(block_table),
+                                         max(_ld(block_table, "block_table"), max_pages), max_pages, _ptr(kv_lens),
+                                         _ptr(cu_q), batch, total_q, int(max_q), float(scale), 1 if causal else 0, int(window),
+                                         _ptr(buf), buf.numel(), _ptr(status), _stream(stream)), "ptq_cache_attention")
 
 
 class LayerBuffers:
