@@ -245,6 +245,7 @@ int ptq_gemm_nt_sliced(double *C, int64_t ldc, const double *A, int64_t lda, con
  * this file hold here too; what these calls add to them:
  *   - `type` parameters name the element type of the caller's activations (ptq_type).
  *   - Calls with nothing to do (no rows, no tokens) return PTQ_OK and launch nothing.
+ *   - An output that shares memory with an input, with the workspace or with another output is refused (PTQ_ERR_INVALID_ARG).
  *   - Sizes that live on the device (lengths, offsets, page and slot numbers) are checked there: an entry that is out of range is
  *     recorded in `status` (PTQ_ERR_INVALID_ARG, index = request or token) and is never used as an address.
  * ------------------------------------------------------------------------------------------------------------------
@@ -307,7 +308,7 @@ size_t ptq_cache_page_bytes(int page_size, int kv_heads, int head_dim);
  *   slots       [max_tokens] int32, out;  positions [max_tokens] int32, out: of the new tokens of request 0, then 1, ...; -1 in both
  *               behind the last token, which ptq_cache_append skips (a batch padded to a fixed size, as a captured graph needs it)
  *   cu_q        [batch + 1] int32, out: first new token of each request, and their number
- *   kv_lens_out [batch] int32, out: kv_lens + new_tokens; must not overlap kv_lens (PTQ_ERR_INVALID_ARG)
+ *   kv_lens_out [batch] int32, out: kv_lens + new_tokens; a buffer of its own, not kv_lens
  *   taken       [1] int32, out: pages taken from the free list
  * If a request does not fit (its table row, max_tokens, num_free, a negative length), status gets PTQ_ERR_INVALID_ARG with the
  * first such request, and nothing is done for any: slots and positions are all -1, cu_q all 0, kv_lens_out = kv_lens, taken 0 and
@@ -328,7 +329,8 @@ int ptq_cache_append(void *pages, int num_pages, int page_size, int kv_heads, in
                      int64_t k_head, const void *v, int64_t v_token, int64_t v_head, int type, const int32_t *slots, int tokens,
                      int32_t *status, void *stream);
 
-/* The values that the cache holds at `slots`, to k and v (as above, written); rows of negative slots are left as they are. */
+/* The values that the cache holds at `slots`, to k and v (as above, written; their elements may alternate in one buffer, but must
+ * differ); rows of negative slots are left as they are. */
 int ptq_cache_read(const void *pages, int num_pages, int page_size, int kv_heads, int head_dim, void *k, int64_t k_token,
                    int64_t k_head, void *v, int64_t v_token, int64_t v_head, int type, const int32_t *slots, int tokens,
                    int32_t *status, void *stream);

@@ -20,6 +20,21 @@ int with_type(int type, F f) {
     return PTQ_ERR_INVALID_ARG;
 }
 
+// Whether an output's bytes [a, a + na) touch an input's (or another output's) [b, b + nb).
+struct Span { const void* p; size_t n; };
+bool touch(Span a, Span b) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+    return a.p && b.p && a.n && b.n && x < y + b.n && y < x + a.n;
+}
+template <typename... S>
+bool touch_any(Span a, S... others) { return (touch(a, others) || ...); }
+Span rows_span(const void* p, int64_t rows, int64_t ld, int64_t cols, int size) {
+    return {p, rows > 0 ? (size_t)((rows - 1) * ld + cols) * size : 0};
+}
+Span heads_span(const void* p, int64_t tokens, int64_t ld_token, int64_t heads, int64_t ld_head, int64_t dim, int size) {
+    return {p, tokens > 0 ? (size_t)((tokens - 1) * ld_token + (heads - 1) * ld_head + dim) * size : 0};
+}
+
 int page_shift_of(int page_size) {
     for (int s = 4; s <= 10; ++s)
         if (page_size == 1 << s) return s;
@@ -155,6 +170,9 @@ int ptq_fp8_quantize(const void* x, int x_type, int rows, int cols, int64_t ldx,
     if (!x || !q || !scale || ldx < cols || ldq < cols || ld_scale < kb) return PTQ_ERR_INVALID_ARG;
     if (cols > 0x7fffff00 || (block_rows > 1 && cdiv(rows, kF8Block) > 65535)) return PTQ_ERR_UNSUPPORTED;
     if (!aligned16(q) || ldq % 16) return PTQ_ERR_ALIGNMENT;
+    const Span in = rows_span(x, rows, ldx, cols, size), codes = rows_span(q, rows, ldq, cols, 1),
+               factors = rows_span(scale, cdiv(rows, block_rows), ld_scale, kb, 4);
+    if (touch_any(codes, in, factors) || touch(factors, in)) return PTQ_ERR_INVALID_ARG;
     const int vec = aligned16(x) && ldx * size % 16 == 0;
     return with_type(x_type, [&](auto* t) {
         using T = std::remove_pointer_t<decltype(t)>;
@@ -185,6 +203,9 @@ int ptq_fp8_matmul(void* C, int c_type, int64_t ldc, const uint8_t* A, int64_t l
         return PTQ_ERR_INVALID_ARG;
     if (k > 0x7fffff00 || (int64_t)cdiv(m, 16) > 65535 || (int64_t)cdiv(n, 128) > 65535) return PTQ_ERR_UNSUPPORTED;
     if (!aligned16(A) || !aligned16(B) || lda % 16 || ldb % 16) return PTQ_ERR_ALIGNMENT;
+    if (touch_any(rows_span(C, m, ldc, n, type_size(c_type)), rows_span(A, m, lda, k, 1), rows_span(B, n, ldb, k, 1),
+                  rows_span(scale_a, m, ld_scale_a, kb, 4), rows_span(scale_b, cdiv(n, kF8Block), ld_scale_b, kb, 4)))
+        return PTQ_ERR_INVALID_ARG;
     DeviceState* dev = nullptr;
     int st = current_device_state(&dev);
     if (st) return st;
@@ -213,7 +234,14 @@ int ptq_cache_plan(const int32_t* kv_lens, const int32_t* new_tokens, int batch,
     if (batch < 0 || max_pages < 0 || ld_table < max_pages || num_free < 0 || max_tokens < 0 || !cu_q || !taken) return PTQ_ERR_INVALID_ARG;
     if (batch > 0 && (!kv_lens || !new_tokens || !kv_lens_out || (max_pages > 0 && !block_table))) return PTQ_ERR_INVALID_ARG;
     if ((num_free > 0 && !free_pages) || (max_tokens > 0 && (!slots || !positions))) return PTQ_ERR_INVALID_ARG;
-    if (batch > 0 && kv_lens_out < kv_lens + batch && kv_lens < kv_lens_out + batch) return PTQ_ERR_INVALID_ARG;     // read by every CTA
+    const size_t per_request = (size_t)batch * 4, per_token = (size_t)max_tokens * 4;
+    const Span lens{kv_lens, per_request}, fresh{new_tokens, per_request}, pages{free_pages, (size_t)num_free * 4},
+        table = rows_span(block_table, max_pages > 0 ? batch : 0, ld_table, max_pages, 4), at{slots, per_token}, pos{positions, per_token},
+        cu{cu_q, per_request + 4}, after{kv_lens_out, per_request}, count{taken, 4};
+    if (touch_any(table, lens, fresh, pages, at, pos, cu, after, count) || touch_any(at, lens, fresh, pages, pos, cu, after, count) ||
+        touch_any(pos, lens, fresh, pages, cu, after, count) || touch_any(cu, lens, fresh, pages, after, count) ||
+        touch_any(after, lens, fresh, pages, count) || touch_any(count, lens, fresh, pages))
+        return PTQ_ERR_INVALID_ARG;                     // every CTA reads what one of them writes for all
     if (shift < 0 || (int64_t)max_pages * page_size > 0x7fffffffll) return PTQ_ERR_UNSUPPORTED;
     CachePlan p{kv_lens, new_tokens, batch, block_table, ld_table, max_pages, free_pages, num_free, shift, slots, positions, max_tokens,
                 cu_q, kv_lens_out, taken, status};
@@ -245,6 +273,10 @@ int ptq_cache_read(const void* pages, int num_pages, int page_size, int kv_heads
     if (tokens < 0 || !type_size(type)) return PTQ_ERR_INVALID_ARG;
     if (tokens == 0) return PTQ_OK;
     if (!k || !v || !slots || k_token < head_dim || k_head < head_dim || v_token < head_dim || v_head < head_dim) return PTQ_ERR_INVALID_ARG;
+    const Span all{pages, (size_t)num_pages * ptq_cache_page_bytes(page_size, kv_heads, head_dim)}, at{slots, (size_t)tokens * 4};
+    if (touch_any(heads_span(k, tokens, k_token, kv_heads, k_head, head_dim, type_size(type)), all, at) ||
+        touch_any(heads_span(v, tokens, v_token, kv_heads, v_head, head_dim, type_size(type)), all, at))
+        return PTQ_ERR_INVALID_ARG;
     return cache_tokens(false, c, head_dim, C4Tokens{k, v, k_token, k_head, v_token, v_head, slots, tokens, 0, status}, type,
                         static_cast<cudaStream_t>(stream_));
 }
@@ -273,6 +305,15 @@ int ptq_cache_attention(void* out, int64_t o_token, int64_t o_head, float* lse, 
     if ((int64_t)max_pages * page_size > 0x7fffffffll || (int64_t)total_q * q_heads > 0x7fffffffll) return PTQ_ERR_UNSUPPORTED;
     if (!aligned16(ws)) return PTQ_ERR_ALIGNMENT;
     if (!ws || ws_bytes < ptq_cache_attention_workspace_bytes(q_heads, kv_heads, head_dim, max_q)) return PTQ_ERR_WORKSPACE;
+    const Span result = heads_span(out, total_q, o_token, q_heads, o_head, head_dim, 2), sums{lse, (size_t)total_q * q_heads * 4},
+               scratch{ws, ptq_cache_attention_workspace_bytes(q_heads, kv_heads, head_dim, max_q)},
+               rows = heads_span(q, total_q, q_token, q_heads, q_head, head_dim, 2),
+               all{pages, (size_t)num_pages * ptq_cache_page_bytes(page_size, kv_heads, head_dim)},
+               table = rows_span(block_table, max_pages > 0 ? batch : 0, ld_table, max_pages, 4), lens{kv_lens, (size_t)batch * 4},
+               cu{cu_q, (size_t)batch * 4 + 4};
+    if (touch_any(result, sums, scratch, rows, all, table, lens, cu) || touch_any(sums, scratch, rows, all, table, lens, cu) ||
+        touch_any(scratch, rows, all, table, lens, cu))
+        return PTQ_ERR_INVALID_ARG;
     DeviceState* dev = nullptr;
     st = current_device_state(&dev);
     if (st) return st;

@@ -370,85 +370,81 @@ def quantize_layer_per_row(W, Hinv, scale, zero, bits, score_mode, codes, What, 
 # on the device of its tensors, whatever the current device is, and on that device's current stream unless one is given.
 # ---------------------------------------------------------------------------------------------------------------------
 _TYPE_IDS = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
+_I32, _F32 = torch.int32, torch.float32
+
+# These calls are short (a plan takes the GPU a few microseconds), so their checks are kept to a few attribute reads a tensor, and
+# what pointers and sizes can tell (memory that an output shares with an input) the library checks itself.
 
 
-def _type_id(t, name, half_only=False):
-    if t.dtype not in _TYPE_IDS or (half_only and t.dtype == torch.float32):
-        raise ValueError(f"{name} must be " + ("" if half_only else "float32, ") + "float16 or bfloat16")
-    return _TYPE_IDS[t.dtype]
+def _expect(ok, message):
+    if not ok:
+        raise ValueError(message)
 
 
-def _ld(t, name):
-    """Row stride of a 2-D tensor with contiguous rows; sizes of 0 and 1 leave strides undefined."""
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1 and t.shape[0] > 0):
-        raise ValueError(f"{name} must be 2-D with unit column stride")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+def _vector(t, n, dev, name):
+    """Pointer of a contiguous int32 vector of n elements on device `dev`."""
+    if t.dtype is not _I32 or t.get_device() != dev or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 vector of {n} on cuda:{dev}, not {t.dtype} {list(t.shape)} on {t.device}")
+    return t.data_ptr()
 
 
-def _strides(t, name):
-    """(token stride, head stride) of [tokens, heads, dim] with contiguous heads, in elements."""
-    tokens, heads, dim = t.shape
-    a, b, c = t.stride()
-    if c != 1 and t.numel():
-        raise ValueError(f"{name} must have unit stride within a head")
-    return a if tokens > 1 else heads * dim, b if heads > 1 else dim
+def _matrix(t, rows, cols, dtype, dev, name):
+    """(pointer, row stride) of a matrix with contiguous rows; sizes of 0 and 1 leave strides undefined."""
+    shape = t.shape
+    if (dtype is not None and t.dtype is not dtype) or t.get_device() != dev or len(shape) != 2 or shape[0] != rows or shape[1] != cols:
+        raise ValueError(f"{name} must be [{rows}, {cols}]" + ("" if dtype is None else f" {dtype}") +
+                         f" on cuda:{dev}, not {t.dtype} {list(shape)} on {t.device}")
+    ld, one = t.stride()
+    if one != 1 and cols > 1 and rows > 0:
+        raise ValueError(f"{name} must have unit column stride")
+    return t.data_ptr(), (ld if rows > 1 else max(ld, cols))
 
 
-def _bytes8(t, name):
-    if t.dtype not in (torch.float8_e4m3fn, torch.uint8):
+def _matrix8(t, rows, cols, dev, name):
+    if t.dtype is not torch.float8_e4m3fn and t.dtype is not torch.uint8:
         raise ValueError(f"{name} must be float8_e4m3fn (or uint8)")
-    return _ld(t, name)
+    return _matrix(t, rows, cols, None, dev, name)
 
 
-def _ints(name, t, shape=None):
-    _dev(t, torch.int32, name)
-    if not t.is_contiguous() or (shape is not None and tuple(t.shape) != tuple(shape)):
-        raise ValueError(f"{name} must be contiguous" + ("" if shape is None else f" {list(shape)}"))
-    return t
+def _heads(t, tokens, heads, dim, dtype, dev, name):
+    """(pointer, token stride, head stride) of [tokens, heads, dim] whose heads are contiguous, strides in elements."""
+    shape = t.shape
+    if t.dtype is not dtype or t.get_device() != dev or len(shape) != 3 or shape[0] != tokens or shape[1] != heads or shape[2] != dim:
+        raise ValueError(f"{name} must be [{tokens}, {heads}, {dim}] {dtype} on cuda:{dev}, not {t.dtype} {list(shape)} on {t.device}")
+    a, b, c = t.stride()
+    if c != 1 and tokens > 0:
+        raise ValueError(f"{name} must have unit stride within a head")
+    return t.data_ptr(), (a if tokens > 1 else heads * dim), (b if heads > 1 else dim)
 
 
-def _shape(name, t, shape):
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must be {list(shape)}, not {list(t.shape)}")
+def _type_id(t, name):
+    i = _TYPE_IDS.get(t.dtype)
+    if i is None:
+        raise ValueError(f"{name} must be float32, float16 or bfloat16, not {t.dtype}")
+    return i
 
 
-def _on_one_device(*tensors):
-    """The device of all these tensors (None among them is skipped)."""
-    dev = None
-    for t in tensors:
-        if t is None:
-            continue
-        if not t.is_cuda:
-            raise ValueError("tensors must be CUDA tensors (the library has no CPU path)")
-        if dev is not None and t.device != dev:
-            raise ValueError(f"tensors are on {dev} and {t.device}: they must share a device")
-        dev = t.device
+def _device_of(t, name):
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError(f"{name} must be a CUDA tensor (the library has no CPU path)")
     return dev
 
 
-def _span(t):
-    """[first, last] byte that a tensor's elements touch."""
-    last = sum((n - 1) * st for n, st in zip(t.shape, t.stride())) * t.element_size()
-    return t.data_ptr(), t.data_ptr() + last + t.element_size() - 1
+def _status_ptr(status, dev):
+    return None if status is None else _vector(status, 4, dev, "status")
 
 
-def _apart(name, out, *inputs):
-    """Refuses an output that shares memory with an input."""
-    if out is None or out.numel() == 0:
-        return
-    a, b = _span(out)
-    for t in inputs:
-        if t is not None and t.numel():
-            c, d = _span(t)
-            if a <= d and c <= b:
-                raise ValueError(f"{name} must not share memory with an input")
-
-
-def _ws_for(ws, nbytes, dev):
-    buf = ws.get(nbytes)
-    if buf.device != dev:
-        raise ValueError(f"the workspace is on {buf.device}, the tensors are on {dev}")
-    return buf
+def _call(fn, dev, stream, *args):
+    """fn(*args, stream) with device `dev` current, on its current stream unless one is given."""
+    raw = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+    if torch.cuda.current_device() == dev:
+        ret = fn(*args, raw)
+    else:
+        with torch.cuda.device(dev):
+            ret = fn(*args, raw)
+    if ret != OK:
+        raise PtqError(ret, fn.__name__)
 
 
 def fp8_empty(rows, cols, device="cuda"):
@@ -459,32 +455,31 @@ def fp8_empty(rows, cols, device="cuda"):
 def fp8_quantize(x, q, scale, status, block_rows=1, stream=None):
     """x [rows, cols] to 8-bit floating point q with a power-of-two scale for each block of block_rows x 128 values (1:
     activations, 128: weights).  q: ``fp8_empty(rows, cols)``, scale: float32 [ceil(rows / block_rows), ceil(cols / 128)]."""
-    dev = _on_one_device(x, q, scale, status)
+    dev = _device_of(x, "x")
+    _expect(x.dim() == 2, "x must be 2-D")
     rows, cols = x.shape
-    _shape("q", q, (rows, cols))
-    _dev(scale, torch.float32, "scale")
-    _shape("scale", scale, (-(-rows // max(1, int(block_rows))), -(-cols // FP8_BLOCK)))
-    _apart("q", q, x); _apart("scale", scale, x)
-    with torch.cuda.device(dev):
-        _check(lib().ptq_fp8_quantize(_ptr(x), _type_id(x, "x"), rows, cols, _ld(x, "x"), int(block_rows), _ptr(q),
-                                      _bytes8(q, "q"), _ptr(scale), _ld(scale, "scale"), _ptr(status), _stream(stream)),
-               "ptq_fp8_quantize")
+    _expect(block_rows == 1 or block_rows == FP8_BLOCK, "block_rows must be 1 or 128")
+    px, ldx = _matrix(x, rows, cols, None, dev, "x")
+    pq, ldq = _matrix8(q, rows, cols, dev, "q")
+    ps, lds = _matrix(scale, -(-rows // block_rows), -(-cols // FP8_BLOCK), _F32, dev, "scale")
+    _call(lib().ptq_fp8_quantize, dev, stream, px, _type_id(x, "x"), rows, cols, ldx, block_rows, pq, ldq, ps, lds,
+          _status_ptr(status, dev))
 
 
 def fp8_matmul(C, A, scale_a, B, scale_b, status, stream=None):
     """C = A B^T for 8-bit floating-point A [m, k] with a scale per row and 128 columns and B [n, k] with one per 128 x 128, as
     ``fp8_quantize`` makes them; C [m, n] float32, float16 or bfloat16."""
-    dev = _on_one_device(C, A, scale_a, B, scale_b, status)
+    dev = _device_of(C, "C")
+    _expect(A.dim() == 2 and B.dim() == 2, "A and B must be 2-D")
     (m, k), n = A.shape, B.shape[0]
-    _shape("B", B, (n, k)); _shape("C", C, (m, n))
-    _dev(scale_a, torch.float32, "scale_a"); _dev(scale_b, torch.float32, "scale_b")
     kb = -(-k // FP8_BLOCK)
-    _shape("scale_a", scale_a, (m, kb)); _shape("scale_b", scale_b, (-(-n // FP8_BLOCK), kb))
-    _apart("C", C, A, scale_a, B, scale_b)
-    with torch.cuda.device(dev):
-        _check(lib().ptq_fp8_matmul(_ptr(C), _type_id(C, "C"), _ld(C, "C"), _ptr(A), _bytes8(A, "A"), _ptr(scale_a),
-                                    _ld(scale_a, "scale_a"), _ptr(B), _bytes8(B, "B"), _ptr(scale_b),
-                                    _ld(scale_b, "scale_b"), m, n, k, _ptr(status), _stream(stream)), "ptq_fp8_matmul")
+    pa, lda = _matrix8(A, m, k, dev, "A")
+    pb, ldb = _matrix8(B, n, k, dev, "B")
+    pc, ldc = _matrix(C, m, n, None, dev, "C")
+    psa, ldsa = _matrix(scale_a, m, kb, _F32, dev, "scale_a")
+    psb, ldsb = _matrix(scale_b, -(-n // FP8_BLOCK), kb, _F32, dev, "scale_b")
+    _call(lib().ptq_fp8_matmul, dev, stream, pc, _type_id(C, "C"), ldc, pa, lda, psa, ldsa, pb, ldb, psb, ldsb, m, n, k,
+          _status_ptr(status, dev))
 
 
 class Cache4:
@@ -499,60 +494,48 @@ class Cache4:
         self.num_pages, self.page_size, self.kv_heads, self.head_dim = num_pages, page_size, kv_heads, head_dim
         if pages is None:
             pages = torch.empty(shape, dtype=torch.uint8, device=device)
-        _dev(pages, torch.uint8, "pages"); _shape("pages", pages, shape)
-        if not pages.is_contiguous():
-            raise ValueError("pages must be contiguous")
+        _dev(pages, torch.uint8, "pages")
+        _expect(tuple(pages.shape) == shape and pages.is_contiguous(), f"pages must be contiguous {list(shape)}")
         self.pages = pages
 
-    def _args(self):
-        return _ptr(self.pages), self.num_pages, self.page_size, self.kv_heads, self.head_dim
+    def _args(self, dev):
+        _expect(self.pages.get_device() == dev, f"the cache is on {self.pages.device}, the tensors are on cuda:{dev}")
+        return self.pages.data_ptr(), self.num_pages, self.page_size, self.kv_heads, self.head_dim
 
 
 def cache_plan(kv_lens, new_tokens, block_table, free_pages, page_size, slots, positions, cu_q, kv_lens_out, taken, status,
                stream=None):
     """Where the new tokens of a batch go: extends ``block_table`` [batch, pages] by pages of ``free_pages``, fills ``slots`` and
-    ``positions`` [tokens] (-1 behind the last token), ``cu_q`` [batch + 1], ``kv_lens_out`` [batch] and ``taken`` [1]; all int32."""
-    dev = _on_one_device(kv_lens, new_tokens, block_table, free_pages, slots, positions, cu_q, kv_lens_out, taken, status)
+    ``positions`` [tokens] (-1 behind the last token), ``cu_q`` [batch + 1], ``kv_lens_out`` [batch] and ``taken`` [1]; all int32,
+    and all apart from one another."""
+    dev = _device_of(slots, "slots")
+    _expect(block_table.dim() == 2, "block_table must be 2-D")
     batch, max_pages = block_table.shape
-    _dev(block_table, torch.int32, "block_table")
-    for name, t in (("kv_lens", kv_lens), ("new_tokens", new_tokens), ("kv_lens_out", kv_lens_out)):
-        _ints(name, t, (batch,))
-    _ints("cu_q", cu_q, (batch + 1,)); _ints("taken", taken, (1,)); _ints("free_pages", free_pages)
-    _ints("slots", slots); _ints("positions", positions, slots.shape)
-    outs = [("block_table", block_table), ("slots", slots), ("positions", positions), ("cu_q", cu_q), ("kv_lens_out", kv_lens_out),
-            ("taken", taken)]
-    for i, (name, t) in enumerate(outs):
-        _apart(name, t, kv_lens, new_tokens, free_pages, *[u for _, u in outs[:i]])
-    with torch.cuda.device(dev):
-        _check(lib().ptq_cache_plan(_ptr(kv_lens), _ptr(new_tokens), batch, int(page_size), _ptr(block_table),
-                                    max(_ld(block_table, "block_table"), max_pages), max_pages, _ptr(free_pages),
-                                    free_pages.numel(), _ptr(slots), _ptr(positions), slots.numel(), _ptr(cu_q),
-                                    _ptr(kv_lens_out), _ptr(taken), _ptr(status), _stream(stream)), "ptq_cache_plan")
+    tokens, num_free = slots.numel(), free_pages.numel()
+    table, ldt = _matrix(block_table, batch, max_pages, _I32, dev, "block_table")
+    _call(lib().ptq_cache_plan, dev, stream, _vector(kv_lens, batch, dev, "kv_lens"), _vector(new_tokens, batch, dev, "new_tokens"), batch,
+          page_size, table, ldt, max_pages, _vector(free_pages, num_free, dev, "free_pages"), num_free,
+          _vector(slots, tokens, dev, "slots"), _vector(positions, tokens, dev, "positions"), tokens,
+          _vector(cu_q, batch + 1, dev, "cu_q"), _vector(kv_lens_out, batch, dev, "kv_lens_out"), _vector(taken, 1, dev, "taken"),
+          _status_ptr(status, dev))
 
 
-def _cache_tokens(fn, where, cache, k, v, slots, status, stream):
-    dev = _on_one_device(cache.pages, k, v, slots, status)
+def _cache_tokens(fn, cache, k, v, slots, status, stream):
+    dev = _device_of(slots, "slots")
     tokens = slots.numel()
-    _ints("slots", slots, (tokens,))
-    for name, t in (("k", k), ("v", v)):
-        _shape(name, t, (tokens, cache.kv_heads, cache.head_dim))
-    if k.dtype != v.dtype:
-        raise ValueError("k and v must have one type")
-    _apart("k", k, cache.pages, slots); _apart("v", v, cache.pages, slots)
-    with torch.cuda.device(dev):
-        _check(fn(*cache._args(), _ptr(k), *_strides(k, "k"), _ptr(v), *_strides(v, "v"), _type_id(k, "k"),
-                  _ptr(slots), tokens, _ptr(status), _stream(stream)), where)
+    shape = tokens, cache.kv_heads, cache.head_dim, k.dtype, dev
+    _call(fn, dev, stream, *cache._args(dev), *_heads(k, *shape, "k"), *_heads(v, *shape, "v"), _type_id(k, "k"),
+          _vector(slots, tokens, dev, "slots"), tokens, _status_ptr(status, dev))
 
 
 def cache_append(cache, k, v, slots, status, stream=None):
     """Writes keys and values [tokens, kv_heads, head_dim] to their ``slots`` (int32, all different; negative ones are skipped)."""
-    _cache_tokens(lib().ptq_cache_append, "ptq_cache_append", cache, k, v, slots, status, stream)
+    _cache_tokens(lib().ptq_cache_append, cache, k, v, slots, status, stream)
 
 
 def cache_read(cache, slots, k, v, status, stream=None):
     """The values held at ``slots`` to k and v [tokens, kv_heads, head_dim]; rows of negative slots stay as they are."""
-    _apart("k", k, v)
-    _cache_tokens(lib().ptq_cache_read, "ptq_cache_read", cache, k, v, slots, status, stream)
+    _cache_tokens(lib().ptq_cache_read, cache, k, v, slots, status, stream)
 
 
 def cache_attention(out, q, cache, block_table, kv_lens, cu_q, max_q, scale, ws, status, causal=True, window=0, lse=None,
@@ -560,28 +543,22 @@ def cache_attention(out, q, cache, block_table, kv_lens, cu_q, max_q, scale, ws,
     """Attention of the newest tokens of each request (rows cu_q[r] .. cu_q[r + 1] - 1 of q [tokens, q_heads, head_dim]) over the
     kv_lens[r] tokens that ``cache`` holds of it.  ``max_q``: the most rows of any request.  ``window`` > 0: a row sees that many
     keys back, itself included.  ``lse``: float32 [tokens, q_heads] for the logarithms of the sums, or None."""
-    dev = _on_one_device(out, q, cache.pages, block_table, kv_lens, cu_q, lse, status)
-    total_q, q_heads, dim = q.shape
-    batch, max_pages = block_table.shape
-    _shape("q", q, (total_q, q_heads, cache.head_dim)); _shape("out", out, q.shape)
-    if q.dtype != out.dtype:
-        raise ValueError("q and out must have one type")
-    _dev(block_table, torch.int32, "block_table")
-    _ints("kv_lens", kv_lens, (batch,)); _ints("cu_q", cu_q, (batch + 1,))
+    dev = _device_of(q, "q")
+    _expect(q.dim() == 3 and block_table.dim() == 2, "q must be 3-D, block_table 2-D")
+    _expect(q.dtype is torch.float16 or q.dtype is torch.bfloat16, "q must be float16 or bfloat16")
+    (tokens, q_heads, _), (batch, max_pages) = q.shape, block_table.shape
+    shape = tokens, q_heads, cache.head_dim, q.dtype, dev
+    table, ldt = _matrix(block_table, batch, max_pages, _I32, dev, "block_table")
+    plse = None
     if lse is not None:
-        _dev(lse, torch.float32, "lse"); _shape("lse", lse, (total_q, q_heads))
-        if not lse.is_contiguous():
-            raise ValueError("lse must be contiguous")
-    _apart("out", out, q, cache.pages, block_table, kv_lens, cu_q, lse)
-    _apart("lse", lse, q, cache.pages, block_table, kv_lens, cu_q)
-    with torch.cuda.device(dev):
-        need = int(lib().ptq_cache_attention_workspace_bytes(q_heads, cache.kv_heads, dim, max(1, int(max_q))))
-        buf = _ws_for(ws, need, dev)
-        _check(lib().ptq_cache_attention(_ptr(out), *_strides(out, "out"), _ptr(lse), _ptr(q), *_strides(q, "q"),
-                                         _type_id(q, "q", half_only=True), q_heads, *cache._args(), _ptr(block_table),
-                                         max(_ld(block_table, "block_table"), max_pages), max_pages, _ptr(kv_lens),
-                                         _ptr(cu_q), batch, total_q, int(max_q), float(scale), 1 if causal else 0, int(window),
-                                         _ptr(buf), buf.numel(), _ptr(status), _stream(stream)), "ptq_cache_attention")
+        plse, ld = _matrix(lse, tokens, q_heads, _F32, dev, "lse")
+        _expect(ld == q_heads, "lse must be contiguous")
+    need = lib().ptq_cache_attention_workspace_bytes(q_heads, cache.kv_heads, cache.head_dim, max(1, max_q))
+    buf = ws.get(need)
+    _expect(buf.get_device() == dev, f"the workspace is on {buf.device}, the tensors are on cuda:{dev}")
+    _call(lib().ptq_cache_attention, dev, stream, *_heads(out, *shape, "out"), plse, *_heads(q, *shape, "q"), _TYPE_IDS[q.dtype], q_heads,
+          *cache._args(dev), table, ldt, max_pages, _vector(kv_lens, batch, dev, "kv_lens"), _vector(cu_q, batch + 1, dev, "cu_q"), batch,
+          tokens, max_q, scale, 1 if causal else 0, window, buf.data_ptr(), buf.numel(), _status_ptr(status, dev))
 
 
 class LayerBuffers:

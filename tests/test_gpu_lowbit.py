@@ -665,15 +665,19 @@ def test_binding_refuses_shared_memory_and_mixed_shapes():
         ptq.fp8_quantize(x, q, torch.empty(4, 2, device="cuda"), st)
     with pytest.raises(ValueError):
         ptq.fp8_matmul(s, q, s, q, s[:1], st)
-    with pytest.raises(ValueError):
-        ptq.fp8_matmul(torch.empty(4, 4, device="cuda"), q, s, q, s, st)
+    with pytest.raises(ptq.PtqError) as e:                       # the scales where the result would go
+        ptq.fp8_matmul(s.view(torch.bfloat16)[:, :1].expand(4, 1), q, s, q[:1], s[:1], st)
+    assert e.value.code == ptq.ERR_INVALID_ARG
     cache = ptq.Cache4(2, 16, 2, 64)
     t = torch.zeros(2, 2, dtype=torch.int32, device="cuda")
     qq = torch.zeros(2, 4, 64, dtype=torch.float16, device="cuda")
     args = (cache, t, t[0], torch.zeros(3, dtype=torch.int32, device="cuda"), 1, 0.1, ptq.Workspace(), st)
-    with pytest.raises(ValueError):
+    with pytest.raises(ptq.PtqError) as e:
         ptq.cache_attention(qq, qq, *args)
+    assert e.value.code == ptq.ERR_INVALID_ARG
     with pytest.raises(ValueError):
         ptq.cache_attention(qq.float(), qq.float() + 1, *args)
+    with pytest.raises(ValueError):                              # three requests' offsets for two
+        ptq.cache_attention(qq + 1, qq, cache, t, t[0], torch.zeros(4, dtype=torch.int32, device="cuda"), 1, 0.1, ptq.Workspace(), st)
     with pytest.raises(ValueError):
-        ptq.cache_plan(t[0], t[0], t, t[0], 16, t[0], t[0], torch.zeros(3, dtype=torch.int32, device="cuda"), t[0], t[0][:1], st)
+        ptq.cache_attention(qq + 1, qq, cache, t.cpu(), *args[2:])

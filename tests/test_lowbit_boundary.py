@@ -9,7 +9,15 @@ import torch
 import lowbit_ref as ref
 from paper_2509_05576_b200 import build as ptq_build
 
-FAKE, ODD = ctypes.c_void_p(4096), ctypes.c_void_p(4100)      # never dereferenced: argument checks come first
+ODD = ctypes.c_void_p((1 << 46) + 4)
+
+
+def at(i):
+    """An address that is never dereferenced (argument checks come first), far from the others."""
+    return ctypes.c_void_p(i << 40)
+
+
+FAKE = at(1)
 
 
 @pytest.fixture(scope="module")
@@ -62,13 +70,13 @@ def test_page_and_workspace_sizes(ptq):
 
 def test_cast_refuses_bad_arguments(ptq):
     f = ptq.lib().ptq_fp8_quantize
-    ok = dict(x=FAKE, x_type=ptq.BF16, rows=4, cols=200, ldx=200, block_rows=1, q=FAKE, ldq=208, scale=FAKE, ld_scale=2, status=FAKE, stream=None)
+    ok = dict(x=at(1), x_type=ptq.BF16, rows=4, cols=200, ldx=200, block_rows=1, q=at(2), ldq=208, scale=at(3), ld_scale=2, status=at(4), stream=None)
 
     def call(**kw):
         return f(*{**ok, **kw}.values())
 
     for kw in (dict(x=None), dict(q=None), dict(scale=None), dict(rows=-1), dict(cols=0), dict(ldx=199), dict(ldq=192), dict(ld_scale=1),
-               dict(x_type=3), dict(x_type=-1), dict(block_rows=64), dict(block_rows=0)):
+               dict(x_type=3), dict(x_type=-1), dict(block_rows=64), dict(block_rows=0), dict(q=at(1)), dict(scale=at(1)), dict(scale=at(2))):
         assert call(**kw) == ptq.ERR_INVALID_ARG, kw
     assert call(ldq=200) == ptq.ERR_ALIGNMENT and call(q=ODD) == ptq.ERR_ALIGNMENT
     assert call(rows=0, x=None, q=None, scale=None) == ptq.OK
@@ -76,14 +84,14 @@ def test_cast_refuses_bad_arguments(ptq):
 
 def test_product_refuses_bad_arguments(ptq):
     f = ptq.lib().ptq_fp8_matmul
-    ok = dict(C=FAKE, c_type=ptq.F32, ldc=100, A=FAKE, lda=208, sa=FAKE, ldsa=2, B=FAKE, ldb=208, sb=FAKE, ldsb=2, m=4, n=100, k=200, status=FAKE,
-              stream=None)
+    ok = dict(C=at(1), c_type=ptq.F32, ldc=100, A=at(2), lda=208, sa=at(3), ldsa=2, B=at(4), ldb=208, sb=at(5), ldsb=2, m=4, n=100, k=200,
+              status=at(6), stream=None)
 
     def call(**kw):
         return f(*{**ok, **kw}.values())
 
     for kw in (dict(C=None), dict(A=None), dict(B=None), dict(sa=None), dict(sb=None), dict(m=-1), dict(n=-1), dict(k=0), dict(ldc=99),
-               dict(lda=192), dict(ldb=192), dict(ldsa=1), dict(ldsb=1), dict(c_type=7)):
+               dict(lda=192), dict(ldb=192), dict(ldsa=1), dict(ldsb=1), dict(c_type=7), dict(C=at(2)), dict(C=at(3)), dict(C=at(4)), dict(C=at(5))):
         assert call(**kw) == ptq.ERR_INVALID_ARG, kw
     for kw in (dict(A=ODD), dict(B=ODD), dict(lda=200), dict(ldb=201)):
         assert call(**kw) == ptq.ERR_ALIGNMENT, kw
@@ -93,17 +101,20 @@ def test_product_refuses_bad_arguments(ptq):
 
 def test_plan_refuses_bad_arguments(ptq):
     f = ptq.lib().ptq_cache_plan
-    vp = ctypes.c_void_p
-    ok = dict(lens=vp(4096), new=vp(8192), batch=4, page=16, table=FAKE, ldt=8, max_pages=8, free=FAKE, num_free=4, slots=FAKE, positions=FAKE,
-              max_tokens=16, cu=FAKE, lens_out=vp(1 << 20), taken=FAKE, status=FAKE, stream=None)
+    ok = dict(lens=at(1), new=at(2), batch=4, page=16, table=at(3), ldt=8, max_pages=8, free=at(4), num_free=4, slots=at(5), positions=at(6),
+              max_tokens=16, cu=at(7), lens_out=at(8), taken=at(9), status=at(10), stream=None)
 
     def call(**kw):
         return f(*{**ok, **kw}.values())
 
     for kw in (dict(lens=None), dict(new=None), dict(table=None), dict(free=None), dict(slots=None), dict(positions=None), dict(cu=None),
                dict(lens_out=None), dict(taken=None), dict(batch=-1), dict(ldt=7), dict(max_pages=-1), dict(num_free=-1), dict(max_tokens=-1),
-               dict(lens_out=vp(4096)), dict(lens_out=vp(4096 + 12))):
+               dict(lens_out=at(1)), dict(lens_out=ctypes.c_void_p((1 << 40) + 12))):
         assert call(**kw) == ptq.ERR_INVALID_ARG, kw
+    outs, ins = ["table", "slots", "positions", "cu", "lens_out", "taken"], ["lens", "new", "free"]
+    for i, name in enumerate(outs):                     # every output lies apart from the inputs and the other outputs
+        for other in ins + outs[:i]:
+            assert call(**{name: ok[other]}) == ptq.ERR_INVALID_ARG, (name, other)
     for kw in (dict(page=8), dict(page=24), dict(page=2048), dict(max_pages=1 << 28, ldt=1 << 28)):
         assert call(**kw) == ptq.ERR_UNSUPPORTED, kw
 
@@ -111,8 +122,8 @@ def test_plan_refuses_bad_arguments(ptq):
 @pytest.mark.parametrize("name", ["ptq_cache_append", "ptq_cache_read"])
 def test_append_and_read_refuse_bad_arguments(ptq, name):
     f = getattr(ptq.lib(), name)
-    ok = dict(pages=FAKE, num_pages=4, page=16, heads=2, dim=64, k=FAKE, kt=128, kh=64, v=FAKE, vt=128, vh=64, type=ptq.F16, slots=FAKE, tokens=3,
-              status=FAKE, stream=None)
+    ok = dict(pages=at(1), num_pages=4, page=16, heads=2, dim=64, k=at(2), kt=128, kh=64, v=at(3), vt=128, vh=64, type=ptq.F16, slots=at(4),
+              tokens=3, status=at(5), stream=None)
 
     def call(**kw):
         return f(*{**ok, **kw}.values())
@@ -126,13 +137,14 @@ def test_append_and_read_refuse_bad_arguments(ptq, name):
     assert call(tokens=0, k=None, v=None, slots=None) == ptq.OK
     if name == "ptq_cache_read":                       # rows that overlap cannot be written
         assert call(kt=32) == ptq.ERR_INVALID_ARG and call(vh=0) == ptq.ERR_INVALID_ARG
+        assert call(k=at(1)) == ptq.ERR_INVALID_ARG and call(v=at(4)) == ptq.ERR_INVALID_ARG
 
 
 def test_attention_refuses_bad_arguments(ptq):
     f = ptq.lib().ptq_cache_attention
-    ok = dict(out=FAKE, ot=512, oh=64, lse=None, q=FAKE, qt=512, qh=64, type=ptq.BF16, q_heads=8, pages=FAKE, num_pages=4, page=16, heads=2, dim=64,
-              table=FAKE, ldt=8, max_pages=8, lens=FAKE, cu=FAKE, batch=2, total=2, max_q=1, scale=0.125, causal=1, window=0, ws=FAKE,
-              ws_bytes=1 << 30, status=FAKE, stream=None)
+    ok = dict(out=at(1), ot=512, oh=64, lse=at(2), q=at(3), qt=512, qh=64, type=ptq.BF16, q_heads=8, pages=at(4), num_pages=4, page=16, heads=2,
+              dim=64, table=at(5), ldt=8, max_pages=8, lens=at(6), cu=at(7), batch=2, total=2, max_q=1, scale=0.125, causal=1, window=0,
+              ws=at(8), ws_bytes=1 << 30, status=at(9), stream=None)
 
     def call(**kw):
         return f(*{**ok, **kw}.values())
@@ -141,6 +153,10 @@ def test_attention_refuses_bad_arguments(ptq):
                dict(q_heads=7), dict(q_heads=0), dict(ldt=7), dict(batch=-1), dict(total=-1), dict(max_q=-1), dict(window=-1), dict(causal=2),
                dict(scale=float("nan")), dict(scale=float("inf")), dict(ot=32), dict(oh=0), dict(qt=-1)):
         assert call(**kw) == ptq.ERR_INVALID_ARG, kw
+    names = ["out", "lse", "ws", "q", "pages", "table", "lens", "cu"]
+    for i, name in enumerate(names[:3]):
+        for other in names[i + 1:]:
+            assert call(**{name: ok[other]}) == ptq.ERR_INVALID_ARG, (name, other)
     for kw in (dict(page=24), dict(dim=96), dict(max_pages=1 << 28, ldt=1 << 28), dict(total=1 << 30)):
         assert call(**kw) == ptq.ERR_UNSUPPORTED, kw
     assert call(pages=ODD) == ptq.ERR_ALIGNMENT and call(ws=ODD) == ptq.ERR_ALIGNMENT
