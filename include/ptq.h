@@ -347,10 +347,10 @@ int ptq_cache_read(const void *pages, int num_pages, int page_size, int kv_heads
  *   block_table, kv_lens, cu_q: as ptq_cache_plan leaves them (kv_lens_out).  Rows behind cu_q[batch] are left as they are.
  *   max_q   the most rows that any request has (it chooses kernels and the workspace; any bound is right, a tight one is fast)
  * Scores, their maximum and sum, and the output are held in float32; the probabilities enter the second product as fp16.
- * Workspace: ptq_cache_attention_workspace_bytes(q_heads, kv_heads, head_dim, max_q) (host function, no CUDA calls); it depends on
- * max_q alone where the other three are given, not on lengths.  Results do not depend on what else runs.
+ * Workspace: ptq_cache_attention_workspace_bytes(q_heads, kv_heads, head_dim, batch, total_q, max_q) (host function, no CUDA
+ * calls; 0 for what is not supported); it does not depend on lengths.
  */
-size_t ptq_cache_attention_workspace_bytes(int q_heads, int kv_heads, int head_dim, int max_q);
+size_t ptq_cache_attention_workspace_bytes(int q_heads, int kv_heads, int head_dim, int batch, int total_q, int max_q);
 int ptq_cache_attention(void *out, int64_t o_token, int64_t o_head, float *lse, const void *q, int64_t q_token, int64_t q_head,
                         int type, int q_heads, const void *pages, int num_pages, int page_size, int kv_heads, int head_dim,
                         const int32_t *block_table, int64_t ld_table, int max_pages, const int32_t *kv_lens, const int32_t *cu_q,

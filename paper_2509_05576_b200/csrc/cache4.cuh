@@ -302,35 +302,42 @@ struct Attn4 {
     int batch, total_q, q_heads, ratio;           // ratio = q_heads / kv_heads
     float scale_log2;                             // scale log2(e)
     int causal, window;
-    int row_limit;                                // requests with more rows (new tokens x ratio) than this are left to the other kernel
+    int row_limit;                                // rows (new tokens x ratio) up to which a request is the business of the kernel for few
+    int q_vec, o_vec;                             // every row of q / of out begins on 16 bytes
     float* partial;
     int32_t* status;
 };
 
-struct AttnRequest {
-    int row0, n, len, rows, tiles, chunk0, chunks;       // tiles of kRows rows; 32- or 64-token chunks from chunk0 on
-    long long units;
-};
-
-template <int kRows, int kChunk>
-__device__ __forceinline__ AttnRequest attn_request(const Attn4& a, int b) {
-    AttnRequest r;
+struct AttnRows { int row0, n, len; };                   // rows row0 .. row0 + n - 1, the last of len tokens
+__device__ __forceinline__ AttnRows attn_rows(const Attn4& a, int b) {
+    AttnRows r;
     const int c0 = a.cu[b], c1 = a.cu[b + 1], len = a.lens[b], most = a.max_pages << a.cache.page_shift;
     r.row0 = min(max(c0, 0), a.total_q);
     r.n = max(min(max(c1, 0), a.total_q) - r.row0, 0);
     r.len = min(max(len, 0), most);
     if (c0 != r.row0 || c1 != r.row0 + r.n || len != r.len) report(a.status, PTQ_ERR_INVALID_ARG, b);
-    r.rows = r.n * a.ratio;
-    if (r.rows > a.row_limit) r.rows = 0;
+    return r;
+}
+
+struct AttnRequest : AttnRows {
+    int rows, tiles, chunk0, chunks;                     // tiles of kRows rows; kChunk-token chunks from chunk0 on
+    long long units;
+};
+template <int kRows, int kChunk>
+__device__ __forceinline__ AttnRequest attn_request(const Attn4& a, int b) {
+    AttnRequest r;
+    static_cast<AttnRows&>(r) = attn_rows(a, b);
+    const long long rows = (long long)r.n * a.ratio;     // at most total_q q_heads < 2^31
+    r.rows = rows > a.row_limit ? 0 : (int)rows;
     r.tiles = (r.rows + kRows - 1) / kRows;
-    const int low = a.window > 0 ? min(max((long long)r.len - r.n - a.window + 1, 0ll), (long long)r.len) : 0;
+    const int low = a.window > 0 ? (int)min(max((long long)r.len - r.n - a.window + 1, 0ll), (long long)r.len) : 0;
     r.chunk0 = low / kChunk;
     r.chunks = max((r.len + kChunk - 1) / kChunk - r.chunk0, 1);          // a request without keys still has rows to write
     r.units = (long long)a.cache.kv_heads * r.tiles * r.chunks;
     return r;
 }
 // Keys [lo, hi) that row token i of the request sees.
-__device__ __forceinline__ void attn_range(const Attn4& a, const AttnRequest& r, int i, int& lo, int& hi) {
+__device__ __forceinline__ void attn_range(const Attn4& a, const AttnRows& r, int i, int& lo, int& hi) {
     const int pos = r.len - r.n + i;
     hi = a.causal ? min(max(pos + 1, 0), r.len) : r.len;
     lo = a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0;
@@ -389,6 +396,10 @@ __device__ __forceinline__ int attn_q_shift(float top) {
 // Probabilities are kept times 2^15 in fp16: down to 2^-29 of the largest they keep all their bits, and nothing above 2^-39 of it
 // is lost, so that many small ones still add up.
 constexpr float kAttnPShift = 15.f;
+// Natural logarithm of a row's sum of exponentials, kept as `sum` of 2^(x - ref + shift).
+__device__ __forceinline__ float attn_lse(float ref, float sum, float shift) {
+    return sum == 0.f ? -INFINITY : (ref + log2f(sum) - shift) * 0.693147180559945309f;
+}
 
 template <typename T> constexpr bool kIsHalf = false;
 template <> constexpr bool kIsHalf<__half> = true;
@@ -442,6 +453,20 @@ __device__ __forceinline__ long long few_scan(long long v, FewScan& s, long long
     __syncthreads();
     return before + x - v;
 }
+// The request that unit u belongs to (s.b) and the units before it (s.before); u < total.
+template <int kRows, int kChunk>
+__device__ __forceinline__ void few_find(const Attn4& a, long long u, FewScan& s) {
+    long long base = 0;
+    for (int first = 0; first < a.batch && base <= u; first += kFewThreads) {
+        const int b = first + threadIdx.x;
+        const long long mine = b < a.batch ? attn_request<kRows, kChunk>(a, b).units : 0;
+        long long all;
+        const long long before = base + few_scan(mine, s, all);
+        if (before <= u && u < before + mine) { s.b = b; s.before = before; }
+        base += all;
+    }
+    __syncthreads();
+}
 __device__ __forceinline__ long long few_share(long long total, int ctas) {
     const long long even = (total + ctas - 1) / ctas;
     return even < kFewWarps ? kFewWarps : even;          // less than a chunk a warp would only add partial results
@@ -479,16 +504,7 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) attn4_few_kernel
     long long u = share * blockIdx.x;
     const long long u_end = min(u + share, total);
     if (u >= total) return;
-    for (long long base = 0, first = 0; first < a.batch; first += kFewThreads) {
-        const int b = (int)first + threadIdx.x;
-        const long long mine = b < a.batch ? attn_request<kRows, F::chunk>(a, b).units : 0;
-        long long all;
-        const long long before = base + few_scan(mine, scan, all);
-        if (before <= u && u < before + mine) { scan.b = b; scan.before = before; }
-        base += all;
-        if (base > u) break;
-    }
-    __syncthreads();
+    few_find<kRows, F::chunk>(a, u, scan);
     int b = scan.b;
     long long before = scan.before;
     unsigned uses = 0;                                   // chunks this warp has asked for so far, over all pieces
@@ -738,7 +754,7 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) attn4_few_kernel
                 T* out = static_cast<T*>(a.out) + (int64_t)(r.row0 + i) * a.o_token + (int64_t)qh * a.o_head + d;
                 out[0] = from_f32<T>(v0 * inv);
                 out[1] = from_f32<T>(v1 * inv);
-                if (d == 0 && a.lse) a.lse[(int64_t)(r.row0 + i) * a.q_heads + qh] = sum == 0.f ? -INFINITY : (ref + log2f(sum) - kAttnPShift) * 0.693147180559945309f;
+                if (d == 0 && a.lse) a.lse[(int64_t)(r.row0 + i) * a.q_heads + qh] = attn_lse(ref, sum, kAttnPShift);
             } else {
                 *reinterpret_cast<float2*>(slot + row * HD + d) = make_float2(v0, v1);
                 if (d == 0) { slot[kRows * HD + row] = top; slot[kRows * (HD + 1) + row] = sum; }
@@ -750,60 +766,45 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) attn4_few_kernel
     }
 }
 
-// Joins the partial results of what several CTAs share: one warp a row.
+// Joins the partial results of what several CTAs share: CTA c looks at the border between the shares of c and c + 1, and if that is
+// the first border inside a row tile, adds up the tile's pieces in their order, a warp a row.
 template <typename T, int HD, int NT>
 __global__ void __launch_bounds__(kFewThreads) attn4_join_kernel(Attn4 a, int ctas) {
     using F = FewShape<HD>;
     constexpr int kRows = 8 * NT, kLane = HD / 32;
     __shared__ FewScan scan;
-    __shared__ long long starts[kFewThreads];
     chained_begin();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const long long total = few_total<kRows, F::chunk>(a, scan), share = few_share(total, ctas);
-    if (share >= total) return;                                   // one CTA had everything
-    const int64_t rh = (int64_t)blockIdx.x * kFewWarps + warp;
-    const int token = (int)(rh / a.q_heads), qh = (int)(rh - (int64_t)token * a.q_heads);
-    int b = -1;
-    long long before = 0;
-    for (long long base = 0, first = 0; first < a.batch; first += kFewThreads) {
-        const int mine_b = (int)first + threadIdx.x;
-        const long long mine = mine_b < a.batch ? attn_request<kRows, F::chunk>(a, mine_b).units : 0;
-        long long all;
-        starts[threadIdx.x] = base + few_scan(mine, scan, all);
-        __syncthreads();
-        for (int i = lane; i < kFewThreads && first + i < a.batch; i += 32)
-            if (a.cu[first + i] <= token && token < a.cu[first + i + 1]) { b = (int)first + i; before = starts[i]; }
-        base += all;
-        __syncthreads();
-    }
-    const unsigned has = __ballot_sync(0xffffffffu, b >= 0);
-    if (token >= a.total_q || !has) return;
-    const int src = __ffs(has) - 1;
-    b = __shfl_sync(0xffffffffu, b, src);
-    before = __shfl_sync(0xffffffffu, before, src);
-    const AttnRequest r = attn_request<kRows, F::chunk>(a, b);
-    if (r.units == 0 || token < r.row0 || token >= r.row0 + r.n) return;
-    const int head = qh / a.ratio, row = (token - r.row0) * a.ratio + qh - head * a.ratio, tile = row / kRows, in = row - tile * kRows;
-    const long long s0 = before + ((long long)head * r.tiles + tile) * r.chunks, s1 = s0 + r.chunks - 1;
+    const long long total = few_total<kRows, F::chunk>(a, scan), share = few_share(total, ctas), u = share * (blockIdx.x + 1);
+    if (u >= total) return;
+    few_find<kRows, F::chunk>(a, u, scan);
+    const AttnRequest r = attn_request<kRows, F::chunk>(a, scan.b);
+    const int seg = (int)((u - scan.before) / r.chunks), head = seg / r.tiles, tile = seg - head * r.tiles;
+    const long long s0 = scan.before + (long long)seg * r.chunks, s1 = s0 + r.chunks - 1;
+    if (s0 == u) return;                                          // a tile begins here
     const int c0 = (int)(s0 / share), c1 = (int)(s1 / share);
-    if (c0 == c1) return;                                         // written whole
-    float top = -INFINITY, sum = 0.f, v[kLane];
+    if (c0 != (int)blockIdx.x) return;                            // an earlier border is the tile's first
+    const int first_row = tile * kRows, live_rows = min(kRows, r.rows - first_row);
+    for (int row = warp; row < live_rows; row += kFewWarps) {
+        float top = -INFINITY, sum = 0.f, v[kLane];
 #pragma unroll
-    for (int i = 0; i < kLane; ++i) v[i] = 0.f;
-    for (int c = c0; c <= c1; ++c) top = fmaxf(top, a.partial[(int64_t)(2 * c + (c == c0)) * few_partial_floats(HD, NT) + kRows * HD + in]);
-    const float ref = top == -INFINITY ? 0.f : top;
-    for (int c = c0; c <= c1; ++c) {
-        const float* slot = a.partial + (int64_t)(2 * c + (c == c0)) * few_partial_floats(HD, NT);
-        const float f = exp2_approx(slot[kRows * HD + in] - ref);
-        sum += f * slot[kRows * (HD + 1) + in];
+        for (int i = 0; i < kLane; ++i) v[i] = 0.f;
+        for (int c = c0; c <= c1; ++c) top = fmaxf(top, a.partial[(int64_t)(2 * c + (c == c0)) * few_partial_floats(HD, NT) + kRows * HD + row]);
+        const float ref = top == -INFINITY ? 0.f : top;
+        for (int c = c0; c <= c1; ++c) {
+            const float* slot = a.partial + (int64_t)(2 * c + (c == c0)) * few_partial_floats(HD, NT);
+            const float f = exp2_approx(slot[kRows * HD + row] - ref);
+            sum += f * slot[kRows * (HD + 1) + row];
 #pragma unroll
-        for (int i = 0; i < kLane; ++i) v[i] += f * slot[in * HD + lane * kLane + i];
+            for (int i = 0; i < kLane; ++i) v[i] += f * slot[row * HD + lane * kLane + i];
+        }
+        const int rr = first_row + row, i0 = rr / a.ratio, qh = head * a.ratio + rr - i0 * a.ratio;
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        T* out = static_cast<T*>(a.out) + (int64_t)(r.row0 + i0) * a.o_token + (int64_t)qh * a.o_head + lane * kLane;
+#pragma unroll
+        for (int i = 0; i < kLane; ++i) out[i] = from_f32<T>(v[i] * inv);
+        if (lane == 0 && a.lse) a.lse[(int64_t)(r.row0 + i0) * a.q_heads + qh] = attn_lse(ref, sum, kAttnPShift);
     }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    T* out = static_cast<T*>(a.out) + (int64_t)token * a.o_token + (int64_t)qh * a.o_head + lane * kLane;
-#pragma unroll
-    for (int i = 0; i < kLane; ++i) out[i] = from_f32<T>(v[i] * inv);
-    if (lane == 0 && a.lse) a.lse[(int64_t)token * a.q_heads + qh] = sum == 0.f ? -INFINITY : (ref + log2f(sum) - kAttnPShift) * 0.693147180559945309f;
 }
 
 }  // namespace ptq

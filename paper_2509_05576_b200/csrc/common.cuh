@@ -210,6 +210,7 @@ enum KernelId {
     K_DGEMM_LOSS, K_SUM_PARTIALS, K_SELFTEST, K_FP64_PROBE, K_DYN_AUX, K_DYN_GATHER,
     K_DGEMM_DYN, K_PER_ROW, K_DGEMM_EQ11, K_X_SLICE, K_X_GEMM, K_FACTOR_SWEEP,
     K_F8_QUANTIZE, K_F8_PRODUCT, K_F8_PRODUCT_FEW, K_CACHE_PLAN, K_CACHE_APPEND, K_CACHE_READ, K_CACHE_ATTN_FEW, K_CACHE_ATTN_JOIN,
+    K_CACHE_ATTN_SCHEDULE, K_CACHE_ATTN_TILE, K_CACHE_ATTN_TILE_JOIN,
     K_COUNT
 };
 
@@ -221,7 +222,7 @@ inline const char* kernel_name(int id) {
         "sweep_coop", "finalize", "dgemm_loss", "sum_partials", "selftest", "fp64_probe", "dyn_aux", "dyn_gather",
         "dgemm_dyn", "per_row", "dgemm_eq11", "x_slice", "i8gemm_tcgen05", "factor_sweep",
         "f8_quantize", "f8_product_tcgen05", "f8_product_few_tcgen05", "cache_plan", "cache_append", "cache_read", "cache_attn_few",
-        "cache_attn_join"};
+        "cache_attn_join", "cache_attn_schedule", "cache_attn_tile_tcgen05", "cache_attn_tile_join"};
     return (id >= 0 && id < K_COUNT) ? names[id] : "unknown";
 }
 

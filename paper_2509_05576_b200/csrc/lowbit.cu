@@ -1,4 +1,5 @@
 // C-ABI entry points of the low-bit serving operators (see include/ptq.h): argument checks and the choice of kernels.
+#include "attn4tile.cuh"
 #include "cache4.cuh"
 #include "common.cuh"
 #include "fp8.cuh"
@@ -136,11 +137,13 @@ cudaError_t allow_attn_smem_all() {
     if (e == cudaSuccess) e = allow_attn_smem<T, 64, 2>();
     if (e == cudaSuccess) e = allow_attn_smem<T, 128, 1>();
     if (e == cudaSuccess) e = allow_attn_smem<T, 128, 2>();
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(attn4_tile_kernel<T, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, TileShape<64>::smem_bytes);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(attn4_tile_kernel<T, 128>, cudaFuncAttributeMaxDynamicSharedMemorySize, TileShape<128>::smem_bytes);
     return e;
 }
 
 template <typename T, int HD, int NT>
-int attn_few_launch(const Attn4& a, int sms, cudaStream_t stream) {
+void attn_few_launch(const Attn4& a, int sms, cudaStream_t stream) {
     const int want = sms * (NT == 1 ? 2 : 1), ctas = want < kFewMaxCtas ? want : kFewMaxCtas;
     {
         Launch l(K_CACHE_ATTN_FEW, stream);
@@ -148,14 +151,67 @@ int attn_few_launch(const Attn4& a, int sms, cudaStream_t stream) {
     }
     {
         Launch l(K_CACHE_ATTN_JOIN, stream);
-        launch_chained(attn4_join_kernel<T, HD, NT>, (unsigned)(((int64_t)a.total_q * a.q_heads + kFewWarps - 1) / kFewWarps),
-                       kFewThreads, 0, stream, a, ctas);
+        launch_chained(attn4_join_kernel<T, HD, NT>, ctas - 1, kFewThreads, 0, stream, a, ctas);
     }
-    return launch_status();
+}
+template <typename T, int HD>
+void attn_tile_launch(const Attn4& a, const TileList& list, int sms, cudaStream_t stream) {
+    const int ctas = sms < kTileMaxCtas ? sms : kTileMaxCtas;
+    {
+        Launch l(K_CACHE_ATTN_SCHEDULE, stream);
+        launch_chained(attn4_schedule_kernel, 1, kScheduleThreads, 0, stream, a, list);
+    }
+    {
+        Launch l(K_CACHE_ATTN_TILE, stream);
+        launch_chained(attn4_tile_kernel<T, HD>, ctas, kTileThreads, TileShape<HD>::smem_bytes, stream, a, list);
+    }
+    {
+        Launch l(K_CACHE_ATTN_TILE_JOIN, stream);
+        launch_chained(attn4_tile_join_kernel<T, HD>, dim3(ctas - 1, 8), 256, 0, stream, a, list, ctas);
+    }
 }
 
-// Rows of one request and kv head that the kernel for few rows takes at once.
-int few_tiles(int64_t rows) { return rows <= 8 ? 1 : 2; }
+// Requests with up to this many rows (new tokens x query heads of a kv head) go to the kernel for few rows, others to the tiles.
+constexpr int kFewRows = 16;
+
+// The pieces of attention's workspace.
+struct AttnSpace {
+    float *few, *tiles;
+    TileList list;
+    size_t bytes;
+};
+AttnSpace attn_space(void* ws, int ratio, int head_dim, int batch, int total_q, int max_q) {
+    AttnSpace s{};
+    Carver cv(ws);
+    const int64_t rows = (int64_t)max_q * ratio;
+    s.few = cv.take<float>((size_t)2 * kFewMaxCtas * few_partial_floats(head_dim, rows <= 8 ? 1 : 2));
+    if (rows > kFewRows) {
+        s.tiles = cv.take<float>((size_t)2 * kTileMaxCtas * tile_partial_floats(head_dim));
+        s.list.most = (int)((int64_t)total_q * ratio / kTileRows) + batch;           // a last, partly filled tile for each request
+        s.list.before = cv.take<long long>((size_t)s.list.most + 2);
+        s.list.tile = cv.take<int2>((size_t)s.list.most);
+    }
+    s.bytes = cv.off;
+    return s;
+}
+
+template <typename T, int HD>
+int attn_launch(Attn4 a, const AttnSpace& space, int max_q, int sms, cudaStream_t stream) {
+    const int64_t rows = (int64_t)max_q * a.ratio;
+    a.partial = space.few;
+    if (rows <= kFewRows) {
+        a.row_limit = 0x7fffffff;
+        if (rows <= 8) attn_few_launch<T, HD, 1>(a, sms, stream);
+        else attn_few_launch<T, HD, 2>(a, sms, stream);
+        return launch_status();
+    }
+    // where every request has max_q rows there are none with few
+    a.row_limit = (int64_t)max_q * a.batch == a.total_q ? 0 : kFewRows;
+    if (a.row_limit > 0) attn_few_launch<T, HD, 2>(a, sms, stream);
+    a.partial = space.tiles;
+    attn_tile_launch<T, HD>(a, space.list, sms, stream);
+    return launch_status();
+}
 
 }  // namespace
 
@@ -281,10 +337,11 @@ int ptq_cache_read(const void* pages, int num_pages, int page_size, int kv_heads
                         static_cast<cudaStream_t>(stream_));
 }
 
-size_t ptq_cache_attention_workspace_bytes(int q_heads, int kv_heads, int head_dim, int max_q) {
-    if (q_heads < 1 || kv_heads < 1 || q_heads % kv_heads || max_q < 1 || (head_dim != 64 && head_dim != 128)) return 0;
-    const int nt = few_tiles((int64_t)max_q * (q_heads / kv_heads));
-    return align_up((size_t)2 * kFewMaxCtas * few_partial_floats(head_dim, nt) * sizeof(float));
+size_t ptq_cache_attention_workspace_bytes(int q_heads, int kv_heads, int head_dim, int batch, int total_q, int max_q) {
+    if (q_heads < 1 || kv_heads < 1 || q_heads % kv_heads || batch < 0 || total_q < 0 || max_q < 0 || (head_dim != 64 && head_dim != 128) ||
+        (int64_t)total_q * q_heads > 0x7fffffffll)
+        return 0;
+    return attn_space(nullptr, q_heads / kv_heads, head_dim, batch, total_q, max_q).bytes;
 }
 
 int ptq_cache_attention(void* out, int64_t o_token, int64_t o_head, float* lse, const void* q, int64_t q_token, int64_t q_head, int type,
@@ -304,9 +361,9 @@ int ptq_cache_attention(void* out, int64_t o_token, int64_t o_head, float* lse, 
         return PTQ_ERR_INVALID_ARG;
     if ((int64_t)max_pages * page_size > 0x7fffffffll || (int64_t)total_q * q_heads > 0x7fffffffll) return PTQ_ERR_UNSUPPORTED;
     if (!aligned16(ws)) return PTQ_ERR_ALIGNMENT;
-    if (!ws || ws_bytes < ptq_cache_attention_workspace_bytes(q_heads, kv_heads, head_dim, max_q)) return PTQ_ERR_WORKSPACE;
+    if (!ws || ws_bytes < ptq_cache_attention_workspace_bytes(q_heads, kv_heads, head_dim, batch, total_q, max_q)) return PTQ_ERR_WORKSPACE;
     const Span result = heads_span(out, total_q, o_token, q_heads, o_head, head_dim, 2), sums{lse, (size_t)total_q * q_heads * 4},
-               scratch{ws, ptq_cache_attention_workspace_bytes(q_heads, kv_heads, head_dim, max_q)},
+               scratch{ws, ptq_cache_attention_workspace_bytes(q_heads, kv_heads, head_dim, batch, total_q, max_q)},
                rows = heads_span(q, total_q, q_token, q_heads, q_head, head_dim, 2),
                all{pages, (size_t)num_pages * ptq_cache_page_bytes(page_size, kv_heads, head_dim)},
                table = rows_span(block_table, max_pages > 0 ? batch : 0, ld_table, max_pages, 4), lens{kv_lens, (size_t)batch * 4},
@@ -327,13 +384,13 @@ int ptq_cache_attention(void* out, int64_t o_token, int64_t o_head, float* lse, 
     a.table = block_table; a.ldt = ld_table; a.max_pages = max_pages; a.lens = kv_lens; a.cu = cu_q;
     a.batch = batch; a.total_q = total_q; a.q_heads = q_heads; a.ratio = q_heads / kv_heads;
     a.scale_log2 = scale * 1.4426950408889634f;
-    a.causal = causal; a.window = window; a.row_limit = 0x7fffffff;
-    a.partial = static_cast<float*>(ws); a.status = status;
-    const int nt = few_tiles((int64_t)max_q * a.ratio);
+    a.causal = causal; a.window = window;
+    a.q_vec = rows_aligned(q, q_token, q_head, 2); a.o_vec = rows_aligned(out, o_token, o_head, 2);
+    a.status = status;
+    const AttnSpace space = attn_space(ws, a.ratio, head_dim, batch, total_q, max_q);
     auto launch = [&](auto* t) {
         using T = std::remove_pointer_t<decltype(t)>;
-        if (head_dim == 64) return nt == 1 ? attn_few_launch<T, 64, 1>(a, dev->sms, stream) : attn_few_launch<T, 64, 2>(a, dev->sms, stream);
-        return nt == 1 ? attn_few_launch<T, 128, 1>(a, dev->sms, stream) : attn_few_launch<T, 128, 2>(a, dev->sms, stream);
+        return head_dim == 64 ? attn_launch<T, 64>(a, space, max_q, dev->sms, stream) : attn_launch<T, 128>(a, space, max_q, dev->sms, stream);
     };
     return type == PTQ_F16 ? launch(static_cast<__half*>(nullptr)) : launch(static_cast<__nv_bfloat16*>(nullptr));
 }

@@ -93,7 +93,7 @@ def lib():
         for name in ("ptq_cache_append", "ptq_cache_read"):
             getattr(L, name).argtypes = [vp, c_int, c_int, c_int, c_int, vp, c_int64, c_int64, vp, c_int64, c_int64, c_int, vp,
                                          c_int, vp, vp]
-        L.ptq_cache_attention_workspace_bytes.argtypes = [c_int, c_int, c_int, c_int]
+        L.ptq_cache_attention_workspace_bytes.argtypes = [c_int] * 6
         L.ptq_cache_attention_workspace_bytes.restype = c_size_t
         L.ptq_cache_attention.argtypes = [vp, c_int64, c_int64, vp, vp, c_int64, c_int64, c_int, c_int, vp, c_int, c_int, c_int,
                                           c_int, vp, c_int64, c_int, vp, vp, c_int, c_int, c_int, c_float, c_int, c_int, vp,
@@ -553,7 +553,7 @@ def cache_attention(out, q, cache, block_table, kv_lens, cu_q, max_q, scale, ws,
     if lse is not None:
         plse, ld = _matrix(lse, tokens, q_heads, _F32, dev, "lse")
         _expect(ld == q_heads, "lse must be contiguous")
-    need = lib().ptq_cache_attention_workspace_bytes(q_heads, cache.kv_heads, cache.head_dim, max(1, max_q))
+    need = lib().ptq_cache_attention_workspace_bytes(q_heads, cache.kv_heads, cache.head_dim, batch, tokens, max_q)
     buf = ws.get(need)
     _expect(buf.get_device() == dev, f"the workspace is on {buf.device}, the tensors are on cuda:{dev}")
     _call(lib().ptq_cache_attention, dev, stream, *_heads(out, *shape, "out"), plse, *_heads(q, *shape, "q"), _TYPE_IDS[q.dtype], q_heads,

@@ -60,9 +60,12 @@ def test_page_and_workspace_sizes(ptq):
     for bad in ((8, 1, 128), (48, 1, 128), (2048, 1, 128), (16, 0, 128), (16, 1, 96), (16, 1, 256), (0, 1, 64)):
         assert size(*bad) == 0
     ws = ptq.lib().ptq_cache_attention_workspace_bytes
-    assert ws(8, 3, 128, 1) == 0 and ws(8, 2, 96, 1) == 0 and ws(8, 2, 128, 0) == 0 and ws(0, 1, 128, 1) == 0
-    need = [ws(32, 8, 128, q) for q in (1, 2, 4, 64, 100000)]
-    assert need == sorted(need) and 0 < need[0] and need[-1] < 64 << 20
+    for bad in ((8, 3, 128, 1, 1, 1), (8, 2, 96, 1, 1, 1), (8, 2, 128, -1, 1, 1), (0, 1, 128, 1, 1, 1), (8, 2, 128, 1, 1 << 30, 1)):
+        assert ws(*bad) == 0
+    # more rows, requests or tokens never need less, and lengths do not enter
+    for need in ([ws(32, 8, 128, 4, 4 * q, q) for q in (1, 2, 4, 5, 64, 100000)], [ws(32, 8, 64, 100, t, 50) for t in (1, 50, 5000)],
+                 [ws(32, 8, 64, b, 5000, 50) for b in (1, 100, 10000)]):
+        assert need == sorted(need) and 0 < need[0] and need[-1] < 128 << 20
     with pytest.raises(ptq.PtqError) as e:
         ptq.Cache4(4, 48, 8, 128)
     assert e.value.code == ptq.ERR_UNSUPPORTED
