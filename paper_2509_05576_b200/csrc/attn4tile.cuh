@@ -18,7 +18,7 @@
 
 namespace ptq {
 
-constexpr int kTileRows = 256, kTileKeys = 128, kTileThreads = 416, kTileMaxCtas = 160, kScheduleThreads = 1024;
+constexpr int kTileRows = 256, kTileKeys = 128, kTileThreads = 512, kTileMaxCtas = 160, kScheduleThreads = 1024;
 constexpr float kTilePShift = 8.f, kTileSlack = 7.f;     // P = 2^(x - ref + 8) <= 2^15
 
 template <int HD> struct TileShape {
@@ -131,20 +131,20 @@ __device__ __forceinline__ void tile_find(const Attn4& a, const TileList& list, 
 
 __host__ __device__ constexpr uint32_t f16_idesc(int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24); }
 __device__ __forceinline__ void tc_mma_f16(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
-    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+    asm volatile("{\n\t.reg .pred p, e;\n\t.reg .b64 da, db;\n\t"
                  "mov.b64 da, {%1, %3};\n\t"
                  "mov.b64 db, {%2, %3};\n\t"
                  "setp.ne.b32 p, %5, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, {%6, %6, %6, %6}, p;\n\t}\n"
+                 "elect.sync _|e, 0xffffffff;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, {%6, %6, %6, %6}, p;\n\t}\n"
                  ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(kF8DescHi), "r"(idesc), "r"(accumulate), "r"(0u)
                  : "memory");
 }
 // The row operand in TMEM, two fp16 a column.
 __device__ __forceinline__ void tc_mma_f16_tmem(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
-    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 db;\n\t"
+    asm volatile("{\n\t.reg .pred p, e;\n\t.reg .b64 db;\n\t"
                  "mov.b64 db, {%2, %3};\n\t"
                  "setp.ne.b32 p, %5, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, {%6, %6, %6, %6}, p;\n\t}\n"
+                 "elect.sync _|e, 0xffffffff;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, {%6, %6, %6, %6}, p;\n\t}\n"
                  ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(kF8DescHi), "r"(idesc), "r"(accumulate), "r"(0u)
                  : "memory");
 }
@@ -157,9 +157,79 @@ __device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t (&r)[16])
 }
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// Loads that stay where they are written: a chunk's are issued before the wait for room, a whole chunk ahead of their use.
+__device__ __forceinline__ uint4 ld_global16(const uint8_t* p) {
+    uint4 v;
+    asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ uint32_t ld_global4(const uint8_t* p) {
+    uint32_t v;
+    asm volatile("ld.global.nc.u32 %0, [%1];" : "=r"(v) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ uint32_t ld_global2(const uint8_t* p) {
+    uint16_t v;
+    asm volatile("ld.global.nc.u16 %0, [%1];" : "=h"(v) : "l"(p));
+    return v;
+}
+
 // Place of 16-byte piece c of row `row` in a K-major operand of `rows` rows, 64 values (128 bytes) a slab, SWIZZLE_128B.
 __device__ __forceinline__ uint32_t tile_at(int rows, int row, int c) {
     return (uint32_t)((c >> 3) * rows * 128 + row * 128 + (((c & 7) ^ (row & 7)) << 4));
+}
+
+// Keys [lo, hi) of a row among the 32 from `at` on, a bit each.
+__device__ __forceinline__ uint32_t tile_seen(int lo, int hi, int at) {
+    const int a = min(max(lo - at, 0), 32), b = min(max(hi - at, 0), 32);
+    return (b == 32 ? 0xffffffffu : (1u << b) - 1u) & ~(a == 32 ? 0xffffffffu : (1u << a) - 1u);
+}
+// A row's largest score of the chunk, and its probabilities, written where the scores were (two fp16 a column), with their sum.
+// kWhole: the row sees all 128 keys; otherwise keys [lo, hi).  The scores are read twice rather than kept in 128 registers.
+template <bool kWhole>
+__device__ __forceinline__ float tile_max(uint32_t s_tmem, int lo, int hi) {
+    float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    uint32_t r[2][32];                                   // 32 scores are read while the 32 before them are looked at
+    tc_ld32(s_tmem, r[0]);
+#pragma unroll
+    for (int ch = 0; ch < 4; ++ch) {
+        const uint32_t seen = kWhole ? 0u : tile_seen(lo, hi, ch * 32);
+        tc_wait_ld();
+        if (ch < 3) tc_ld32(s_tmem + (ch + 1) * 32, r[(ch + 1) & 1]);
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+            const float v = kWhole || (seen >> e & 1u) ? __uint_as_float(r[ch & 1][e]) : -INFINITY;
+            top[e & 3] = fmaxf(top[e & 3], v);
+        }
+    }
+    return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+}
+template <bool kWhole>
+__device__ __forceinline__ float tile_probs(uint32_t s_tmem, float mult, float off, int lo, int hi) {
+    float part[4] = {0.f, 0.f, 0.f, 0.f};
+    uint32_t r[2][32];
+    tc_ld32(s_tmem, r[0]);
+#pragma unroll
+    for (int ch = 0; ch < 4; ++ch) {
+        uint32_t w[16];
+        const uint32_t seen = kWhole ? 0u : tile_seen(lo, hi, ch * 32);
+        tc_wait_ld();
+        if (ch < 3) tc_ld32(s_tmem + (ch + 1) * 32, r[(ch + 1) & 1]);
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) {
+            float v0 = exp2_approx(fmaf(__uint_as_float(r[ch & 1][e]), mult, off));
+            float v1 = exp2_approx(fmaf(__uint_as_float(r[ch & 1][e + 1]), mult, off));
+            if (!kWhole) {
+                v0 = seen >> e & 1u ? v0 : 0.f;
+                v1 = seen >> (e + 1) & 1u ? v1 : 0.f;
+            }
+            part[e & 3] += v0;
+            part[(e & 3) + 1] += v1;
+            w[e >> 1] = pack_half2(v0, v1);
+        }
+        tc_st16(s_tmem + ch * 16, w);
+    }
+    return (part[0] + part[1]) + (part[2] + part[3]);
 }
 
 template <typename T, int HD>
@@ -180,7 +250,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn4_tile_kernel(Attn4 a, Ti
     auto o_full = [&](int t) { return bar0 + 8u * (10 + t); };
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tail + 8 * 12);
     volatile int* abort_flag = &abort_word;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(q_full(i), 128);
@@ -199,7 +269,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn4_tile_kernel(Attn4 a, Ti
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *tmem_slot;
+    const uint32_t tmem = (uint32_t)uniform((int)*tmem_slot);
     chained_wait();
 
     const int count = (int)list.before[list.most + 1];
@@ -214,6 +284,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn4_tile_kernel(Attn4 a, Ti
 
     if (warp < 8) {
         // ------------------------------------------------------------ softmax: a row a thread
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
         const int t = warp >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, s_tmem = tmem + lanes + t * 128, o_tmem = tmem + lanes + 256 + t * 128;
         unsigned char* q_smem = base_ptr + t * (S::q_bytes / 2);
@@ -263,23 +334,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn4_tile_kernel(Attn4 a, Ti
                 tc_fence_after();
                 const int j0 = (p.range.chunk0 + c) * kTileKeys;
                 const bool whole = j0 >= p.range.lo_all && j0 + kTileKeys <= p.range.hi_all;
-                float top = -INFINITY;
-#pragma unroll
-                for (int ch = 0; ch < 4; ++ch) {
-                    uint32_t r[32];
-                    tc_ld32(s_tmem + ch * 32, r);
-                    tc_wait_ld();
-                    if (whole) {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) top = fmaxf(top, __uint_as_float(r[e]));
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            const int j = j0 + ch * 32 + e;
-                            if (j >= lo && j < hi) top = fmaxf(top, __uint_as_float(r[e]));
-                        }
-                    }
-                }
+                float top = (whole ? tile_max<true>(s_tmem, 0, 0) : tile_max<false>(s_tmem, lo - j0, hi - j0));
                 top *= mult;
                 const bool move = top > ref + kTileSlack || (ref == -INFINITY && top > ref);
                 if (__any_sync(0xffffffffu, move)) {
@@ -298,27 +353,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn4_tile_kernel(Attn4 a, Ti
                     }
                 }
                 const float off = kTilePShift - (ref == -INFINITY ? 0.f : ref);
-                float part[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int ch = 0; ch < 4; ++ch) {
-                    uint32_t r[32], w[16];
-                    tc_ld32(s_tmem + ch * 32, r);
-                    tc_wait_ld();
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        float v = exp2_approx(fmaf(__uint_as_float(r[e]), mult, off));
-                        if (!whole) {
-                            const int j = j0 + ch * 32 + e;
-                            if (j < lo || j >= hi) v = 0.f;
-                        }
-                        part[e & 3] += v;
-                        r[e] = __float_as_uint(v);
-                    }
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) w[e] = pack_half2(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1]));
-                    tc_st16(s_tmem + ch * 16, w);
-                }
-                sum += (part[0] + part[1]) + (part[2] + part[3]);
+                sum += whole ? tile_probs<true>(s_tmem, mult, off, 0, 0) : tile_probs<false>(s_tmem, mult, off, lo - j0, hi - j0);
                 tc_wait_st();
                 tc_fence_before();
                 mbar_arrive(p_full(t));
@@ -351,6 +386,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn4_tile_kernel(Attn4 a, Ti
         if (!ok && lane == 0) *abort_flag = 1;
     } else if (warp < 12) {
         // ------------------------------------------------------------ unpacking
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 112;");
         constexpr int kK = HD / 32, kV = HD / 64;              // 16-byte pieces: a key; half a value
         const int u = threadIdx.x - 256, half = (warp - 8) & 1, dims = (warp - 8) >> 1, pair = half * 64 + 2 * lane;
         struct Raw { uint4 k[kK], v[2][kV]; uint32_t kg[kK / 2], vg[2]; } now, ahead;
@@ -366,9 +402,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn4_tile_kernel(Attn4 a, Ti
             const uint8_t* kt = tile_of(j0 + u);
             const int kr = (j0 + u) & 15;
 #pragma unroll
-            for (int e = 0; e < kK; ++e) x.k[e] = kt ? __ldg(reinterpret_cast<const uint4*>(kt + kr * (HD / 2)) + e) : make_uint4(0, 0, 0, 0);
+            for (int e = 0; e < kK; ++e) x.k[e] = kt ? ld_global16(kt + kr * (HD / 2) + 16 * e) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-            for (int e = 0; e < kK / 2; ++e) x.kg[e] = kt ? __ldg(reinterpret_cast<const uint32_t*>(kt + kCodes + kr * kGrids) + e) : 0u;
+            for (int e = 0; e < kK / 2; ++e) x.kg[e] = kt ? ld_global4(kt + kCodes + kr * kGrids + 4 * e) : 0u;
             const uint8_t* vt = tile_of(j0 + pair);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -376,11 +412,11 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn4_tile_kernel(Attn4 a, Ti
                 const uint8_t* side = vt + kSide;
 #pragma unroll
                 for (int e = 0; e < kV; ++e)
-                    x.v[h][e] = vt ? __ldg(reinterpret_cast<const uint4*>(side + vr * (HD / 2) + dims * (HD / 4)) + e) : make_uint4(0, 0, 0, 0);
+                    x.v[h][e] = vt ? ld_global16(side + vr * (HD / 2) + dims * (HD / 4) + 16 * e) : make_uint4(0, 0, 0, 0);
                 // what nobody sees may hold anything: 0 times it has to be 0
                 const bool seen = vt && j >= q.range.lo_any && j < q.range.hi_any;
-                if constexpr (HD == 128) x.vg[h] = seen ? __ldg(reinterpret_cast<const uint32_t*>(side + kCodes + vr * kGrids) + dims) : 0u;
-                else x.vg[h] = seen ? (uint32_t)__ldg(reinterpret_cast<const uint16_t*>(side + kCodes + vr * kGrids) + dims) : 0u;
+                if constexpr (HD == 128) x.vg[h] = seen ? ld_global4(side + kCodes + vr * kGrids + 4 * dims) : 0u;
+                else x.vg[h] = seen ? ld_global2(side + kCodes + vr * kGrids + 2 * dims) : 0u;
             }
         };
         auto unpack = [&](unsigned char* stage, const Raw& x) {
@@ -431,7 +467,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn4_tile_kernel(Attn4 a, Ti
                 if (++stage == 2) { stage = 0; phase ^= 1u; }
             }
         }
-    } else if (lane == 0) {
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        if (warp == 12) {
         // ------------------------------------------------------------ products
         int stage = 0;
         uint32_t kv_phase = 0, q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
@@ -443,14 +481,14 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn4_tile_kernel(Attn4 a, Ti
                 const uint32_t at = (ks >> 2) * (128 * 128 >> 4) + (ks & 3) * 2;
                 tc_mma_f16(tmem + t * 128, qa + at, kb + at, f16_idesc(kTileKeys), ks > 0);
             }
-            tc_commit(s_full(t));
+            tc_commit_elected(s_full(t));
         };
         while (ok && walk.next(a, list, p)) {
             const bool two = p.r.n * a.ratio - p.tile * kTileRows > 128;
             const int tiles = two ? 2 : 1;
-            ok = mbar_wait_bounded(kv_full(stage), kv_phase, abort_flag);
+            ok = __all_sync(0xffffffffu, mbar_wait_bounded(kv_full(stage), kv_phase, abort_flag));
             for (int t = 0; t < tiles && ok; ++t) {
-                ok = mbar_wait_bounded(q_full(t), q_phase[t], abort_flag);
+                ok = __all_sync(0xffffffffu, mbar_wait_bounded(q_full(t), q_phase[t], abort_flag));
                 if (!ok) break;
                 q_phase[t] ^= 1u;
                 tc_fence_after();
@@ -461,7 +499,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn4_tile_kernel(Attn4 a, Ti
                 const uint32_t next_phase = kv_phase ^ (stage == 1 ? 1u : 0u);
                 const bool more = c + 1 < p.to;
                 for (int t = 0; t < tiles; ++t) {
-                    ok = mbar_wait_bounded(p_full(t), p_phase[t], abort_flag);
+                    ok = __all_sync(0xffffffffu, mbar_wait_bounded(p_full(t), p_phase[t], abort_flag));
                     if (!ok) break;
                     p_phase[t] ^= 1u;
                     tc_fence_after();
@@ -470,21 +508,22 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn4_tile_kernel(Attn4 a, Ti
                     for (int ks = 0; ks < kTileKeys / 16; ++ks)
                         tc_mma_f16_tmem(tmem + 256 + t * 128, tmem + t * 128 + ks * 8, vb + (ks >> 2) * (HD * 128 >> 4) + (ks & 3) * 2, f16_idesc(HD),
                                         c > p.from || ks > 0);
-                    if (t == tiles - 1) tc_commit(kv_empty(stage));
+                    if (t == tiles - 1) tc_commit_elected(kv_empty(stage));
                     if (more) {
                         if (t == 0) {
-                            ok = mbar_wait_bounded(kv_full(next), next_phase, abort_flag);
+                            ok = __all_sync(0xffffffffu, mbar_wait_bounded(kv_full(next), next_phase, abort_flag));
                             if (!ok) break;
                             tc_fence_after();
                         }
                         scores(t, next);
                     } else {
-                        tc_commit(o_full(t));
+                        tc_commit_elected(o_full(t));
                     }
                 }
                 stage = next;
                 kv_phase = next_phase;
             }
+        }
         }
     }
     tc_fence_before();

@@ -84,36 +84,42 @@ __device__ __forceinline__ longlong2 plan_scan(longlong2 v, longlong2* warp_sums
     return make_longlong2(before.x + x.x - v.x, before.y + x.y - v.y);
 }
 
-// One launch.  Every CTA scans all requests (a thousand at a time) and answers for kPlanTokens tokens; the first one also writes
-// what belongs to requests.  Nothing is written before the whole batch is known to fit: a batch that does not leaves every slot at
-// -1, no rows (cu = 0), the lengths as they were and the table untouched.  A new page's first token is always new, so that the
-// token writes the page's table entry.
+// One launch.  Every CTA scans all requests (a thousand at a time) and answers for kPlanTokens tokens, four a thread, each of which
+// finds its request by bisection; the first CTA also writes what belongs to requests.  Nothing is written before the whole batch is
+// known to fit: a batch that does not leaves every slot at -1, no rows (cu = 0), the lengths as they were and the table untouched.
+// A new page's first token is always new, so that the token writes the page's table entry.
+struct PlanRequest { int len, n, have, want; bool ok; };
+__device__ __forceinline__ PlanRequest plan_request(const CachePlan& p, int b) {
+    PlanRequest r{0, 0, 0, 0, true};
+    if (b >= p.batch) return r;
+    const int ps = 1 << p.page_shift;
+    r.len = p.lens[b];
+    r.n = p.fresh[b];
+    if (r.len < 0 || r.n < 0 || (long long)r.len + r.n > 0x7fffffffll - ps) return PlanRequest{0, 0, 0, 0, false};
+    r.have = (r.len + ps - 1) >> p.page_shift;
+    r.want = (r.len + r.n + ps - 1) >> p.page_shift;
+    r.ok = r.want <= p.max_pages;
+    return r;
+}
+
 __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(CachePlan p) {
     chained_begin();
     __shared__ longlong2 warp_sums[32];
     __shared__ int bad_request;
-    const int lane = threadIdx.x & 31, ps = 1 << p.page_shift;
-    const long long t0 = (long long)blockIdx.x * kPlanTokens, t1 = t0 + kPlanTokens;
+    __shared__ int at_token[kPlanThreads], at_page[kPlanThreads], at_len[kPlanThreads], at_have[kPlanThreads];
+    const int ps = 1 << p.page_shift;
+    const long long t0 = (long long)blockIdx.x * kPlanTokens, t1 = min(t0 + kPlanTokens, (long long)p.max_tokens);
     if (threadIdx.x == 0) bad_request = 0x7fffffff;
     __syncthreads();
-    auto request = [&](int b, int& len, int& n, int& have, int& want) {
-        len = n = have = want = 0;
-        if (b >= p.batch) return true;
-        len = p.lens[b];
-        n = p.fresh[b];
-        if (len < 0 || n < 0 || (long long)len + n > 0x7fffffffll - ps) { len = n = 0; return false; }
-        have = (len + ps - 1) >> p.page_shift;
-        want = (len + n + ps - 1) >> p.page_shift;
-        return want <= p.max_pages;
-    };
     long long tokens = 0, pages = 0;
+    PlanRequest r;
+    longlong2 at, all;
     for (int first = 0; first < p.batch; first += kPlanThreads) {
-        int len, n, have, want;
         const int b = first + threadIdx.x;
-        const bool ok = request(b, len, n, have, want);
-        longlong2 all;
-        const longlong2 at = plan_scan(make_longlong2(n, want - have), warp_sums, all);
-        if (b < p.batch && (!ok || tokens + at.x + n > p.max_tokens || pages + at.y + want - have > p.num_free)) atomicMin(&bad_request, b);
+        r = plan_request(p, b);
+        at = plan_scan(make_longlong2(r.n, r.want - r.have), warp_sums, all);
+        if (!r.ok || (b < p.batch && (tokens + at.x + r.n > p.max_tokens || pages + at.y + r.want - r.have > p.num_free)))
+            atomicMin(&bad_request, b);
         tokens += all.x;
         pages += all.y;
     }
@@ -126,55 +132,47 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(CachePlan p) {
         if (!fits) report(p.status, PTQ_ERR_INVALID_ARG, bad);
     }
     const long long used = fits ? tokens : 0;
-    for (long long t = t0 + threadIdx.x; t < t1 && t < p.max_tokens; t += kPlanThreads)
-        if (t >= used) { p.slots[t] = -1; p.positions[t] = -1; }
+    for (long long t = max(t0, used) + threadIdx.x; t < t1; t += kPlanThreads) { p.slots[t] = -1; p.positions[t] = -1; }
     if (!fits) {
         if (blockIdx.x == 0)
             for (int b = threadIdx.x; b < p.batch; b += kPlanThreads) { p.cu[b + 1] = 0; p.lens_out[b] = p.lens[b]; }
         return;
     }
+    const bool again = p.batch > kPlanThreads;            // otherwise this thread's request is still at hand
     tokens = pages = 0;
     for (int first = 0; first < p.batch; first += kPlanThreads) {
-        int len, n, have, want;
         const int b = first + threadIdx.x;
-        request(b, len, n, have, want);
-        longlong2 all;
-        longlong2 at = plan_scan(make_longlong2(n, want - have), warp_sums, all);
-        at.x += tokens;
-        at.y += pages;
-        tokens += all.x;
-        pages += all.y;
-        if (b < p.batch && blockIdx.x == 0) { p.cu[b + 1] = (int)(at.x + n); p.lens_out[b] = len + n; }
-        // the warp takes the requests of its lanes that have tokens here one after the other, 32 tokens at a time; where each
-        // has one token only, every lane takes its own
-        const bool mine = n > 0 && at.x < t1 && at.x + n > t0;
-        const bool single = __all_sync(0xffffffffu, n <= 1);
-        unsigned todo = __ballot_sync(0xffffffffu, mine);
-        if (single && !mine) todo = 0;
-        if (single && mine) todo = 1u << lane;
-        while (todo) {
-            const int src = __ffs(todo) - 1;
-            todo &= todo - 1;
-            int rb = b, rlen = len, rn = n, rhave = have, rat = (int)at.x, rpage = (int)at.y;
-            if (!single) {
-                rb = __shfl_sync(0xffffffffu, b, src); rlen = __shfl_sync(0xffffffffu, len, src);
-                rn = __shfl_sync(0xffffffffu, n, src); rhave = __shfl_sync(0xffffffffu, have, src);
-                rat = __shfl_sync(0xffffffffu, (int)at.x, src); rpage = __shfl_sync(0xffffffffu, (int)at.y, src);
-            }
-            int32_t* row = p.table + (int64_t)rb * p.ldt;
-            const int lo = t0 > rat ? (int)(t0 - rat) : 0, hi = t1 < (long long)rat + rn ? (int)(t1 - rat) : rn;
-            for (int i = lo + (single ? 0 : lane); i < hi; i += single ? 1 : 32) {
-                const int pos = rlen + i, pi = pos >> p.page_shift;
-                const int page = pi >= rhave ? p.free_pages[rpage + pi - rhave] : row[pi];
-                if (pi >= rhave && (pos & (ps - 1)) == 0) row[pi] = page;
+        if (again) {
+            r = plan_request(p, b);
+            at = plan_scan(make_longlong2(r.n, r.want - r.have), warp_sums, all);
+        }
+        if (b < p.batch && blockIdx.x == 0) { p.cu[b + 1] = (int)(tokens + at.x + r.n); p.lens_out[b] = r.len + r.n; }
+        const long long lo = max(t0, tokens), hi = min(t1, tokens + all.x);
+        if (lo < hi) {                                    // the same for all threads
+            at_token[threadIdx.x] = (int)(tokens + at.x);
+            at_page[threadIdx.x] = (int)(pages + at.y);
+            at_len[threadIdx.x] = r.len;
+            at_have[threadIdx.x] = r.have;
+            __syncthreads();
+            for (long long t = lo + threadIdx.x; t < hi; t += kPlanThreads) {
+                int i = 0;                                // the last request that begins at or before t: those behind it have tokens later
+#pragma unroll
+                for (int step = kPlanThreads / 2; step > 0; step >>= 1)
+                    if (at_token[i + step] <= (int)t) i += step;
+                const int pos = at_len[i] + (int)t - at_token[i], pi = pos >> p.page_shift, have = at_have[i];
+                int32_t* row = p.table + (int64_t)(first + i) * p.ldt;
+                const int page = pi >= have ? p.free_pages[at_page[i] + pi - have] : row[pi];
+                if (pi >= have && (pos & (ps - 1)) == 0) row[pi] = page;
                 const long long slot = ((long long)page << p.page_shift) + (pos & (ps - 1));
                 const bool ok = page >= 0 && slot <= 0x7fffffffll;
-                if (!ok) report(p.status, PTQ_ERR_INVALID_ARG, rb, 1);
-                p.slots[rat + i] = ok ? (int)slot : -1;
-                p.positions[rat + i] = pos;
+                if (!ok) report(p.status, PTQ_ERR_INVALID_ARG, first + i, 1);
+                p.slots[t] = ok ? (int)slot : -1;
+                p.positions[t] = pos;
             }
+            __syncthreads();
         }
-        __syncwarp();
+        tokens += all.x;
+        pages += all.y;
     }
 }
 

@@ -173,12 +173,13 @@ constexpr uint32_t kF8DescLo = 1u << 16;
 // e4m3 x e4m3 -> float32, M = 128.
 __host__ __device__ constexpr uint32_t f8_idesc(int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24); }
 
+// The whole warp; one lane issues.
 __device__ __forceinline__ void tc_mma_f8(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
-    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+    asm volatile("{\n\t.reg .pred p, e;\n\t.reg .b64 da, db;\n\t"
                  "mov.b64 da, {%1, %3};\n\t"
                  "mov.b64 db, {%2, %3};\n\t"
                  "setp.ne.b32 p, %5, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], da, db, %4, {%6, %6, %6, %6}, p;\n\t}\n"
+                 "elect.sync _|e, 0xffffffff;\n\t@e tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], da, db, %4, {%6, %6, %6, %6}, p;\n\t}\n"
                  ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(kF8DescHi), "r"(idesc), "r"(accumulate), "r"(0u)
                  : "memory");
 }
@@ -211,7 +212,7 @@ __device__ __forceinline__ void store_row16(T* p, const float* v, int n, bool ve
 // issues the four MMAs of a block into one of two TMEM buffers; eight epilogue warps drain the other, one row of the tile and
 // 128 columns a thread, and join it to their float32 sums.  128 x 256 x 128 takes the tensor cores 512 clocks, the epilogue's
 // 128 FMAs and 4 TMEM reads a thread about 350 issue slots of each scheduler.
-constexpr int kF8TileM = 128, kF8TileN = 256, kF8Stages = 4, kF8Threads = 320;
+constexpr int kF8TileM = 128, kF8TileN = 256, kF8Stages = 4, kF8Threads = 384;
 constexpr int kF8StageBytes = (kF8TileM + kF8TileN) * kF8Block;
 constexpr int kF8SmemBytes = 1024 + kF8Stages * kF8StageBytes + 256;
 constexpr int kF8GroupM = 16;                 // tiles are taken in groups of this many row blocks, so that a wave shares columns in L2
@@ -238,7 +239,7 @@ f8_product_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constan
     auto acc_empty = [&](int b) { return bar0 + 8u * (2 * kF8Stages + 2 + b); };
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tail + 8 * (2 * kF8Stages + 4));
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tiles = tiles_m * tiles_n;
+    const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31, tiles = tiles_m * tiles_n;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kF8Stages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
@@ -251,8 +252,11 @@ f8_product_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constan
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *tmem_slot;
+    const uint32_t tmem = (uint32_t)uniform((int)*tmem_slot);
 
+    // registers: eight epilogue warps with 128 sums each want more than a third of them
+    if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == 0) {
         if (lane == 0) {
             int stage = 0, armed[kF8Stages];
@@ -280,30 +284,29 @@ f8_product_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constan
             }
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            int stage = 0, buf = 0;
-            uint32_t phase = 0, acc_phase = 0;
-            bool ok = true;
-            for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
-                for (int b = 0; b < p.kb && ok; ++b) {
-                    ok = mbar_wait_bounded(acc_empty(buf), acc_phase ^ 1u, abort_flag) &&
-                         mbar_wait_bounded(full_bar(stage), phase, abort_flag);
-                    if (!ok) break;
-                    tc_fence_after();
-                    const uint32_t a = kF8DescLo + ((base + stage * kF8StageBytes) >> 4);
+        int stage = 0, buf = 0;
+        uint32_t phase = 0, acc_phase = 0;
+        bool ok = true;
+        for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
+            for (int b = 0; b < p.kb && ok; ++b) {
+                ok = __all_sync(0xffffffffu, mbar_wait_bounded(acc_empty(buf), acc_phase ^ 1u, abort_flag) &&
+                                                 mbar_wait_bounded(full_bar(stage), phase, abort_flag));
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t a = kF8DescLo + ((base + stage * kF8StageBytes) >> 4);
 #pragma unroll
-                    for (int ks = 0; ks < 4; ++ks)
-                        tc_mma_f8(tmem + buf * kF8TileN, a + 2 * ks, a + 2 * ks + (kF8TileM * kF8Block >> 4), f8_idesc(kF8TileN),
-                                  ks > 0);
-                    tc_commit(empty_bar(stage));
-                    tc_commit(acc_full(buf));
-                    if (++stage == kF8Stages) { stage = 0; phase ^= 1u; }
-                    if (++buf == 2) { buf = 0; acc_phase ^= 1u; }
-                }
+                for (int ks = 0; ks < 4; ++ks)
+                    tc_mma_f8(tmem + buf * kF8TileN, a + 2 * ks, a + 2 * ks + (kF8TileM * kF8Block >> 4), f8_idesc(kF8TileN), ks > 0);
+                tc_commit_elected(empty_bar(stage));
+                tc_commit_elected(acc_full(buf));
+                if (++stage == kF8Stages) { stage = 0; phase ^= 1u; }
+                if (++buf == 2) { buf = 0; acc_phase ^= 1u; }
             }
         }
+    }
     } else {
-        const int quarter = warp & 3, half = (warp - 2) >> 2;
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        const int quarter = warp & 3, half = (warp - 4) >> 2;
         int buf = 0;
         uint32_t acc_phase = 0;
         bool ok = true;
@@ -326,16 +329,21 @@ f8_product_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constan
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + buf * kF8TileN + half * kF8Block;
+                // 32 columns are read while the 32 before them are added
+                uint32_t r[2][32];
+                tc_ld32(taddr, r[0]);
 #pragma unroll
                 for (int ch = 0; ch < kF8Block / 32; ++ch) {
-                    uint32_t r[32];
-                    tc_ld32(taddr + ch * 32, r);
                     tc_wait_ld();
+                    if (ch + 1 < kF8Block / 32) {
+                        tc_ld32(taddr + (ch + 1) * 32, r[(ch + 1) & 1]);
+                    } else {
+                        tc_fence_before();
+                        mbar_arrive(acc_empty(buf));
+                    }
 #pragma unroll
-                    for (int c = 0; c < 32; ++c) acc[ch * 32 + c] = fmaf(s, __uint_as_float(r[c]), acc[ch * 32 + c]);
+                    for (int c = 0; c < 32; ++c) acc[ch * 32 + c] = fmaf(s, __uint_as_float(r[ch & 1][c]), acc[ch * 32 + c]);
                 }
-                tc_fence_before();
-                mbar_arrive(acc_empty(buf));
                 if (++buf == 2) { buf = 0; acc_phase ^= 1u; }
             }
             if (ok && live) {
@@ -383,7 +391,7 @@ f8_product_few_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_con
     auto acc_empty = [&](int b) { return bar0 + 8u * (2 * F::stages + F::bufs + b); };
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tail + 8 * (2 * F::stages + 2 * F::bufs));
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const int rank = blockIdx.x, col0 = blockIdx.y * 128, row0 = blockIdx.z * NT;
     const int b0 = (int)((int64_t)p.kb * rank / ks_count), b1 = (int)((int64_t)p.kb * (rank + 1) / ks_count);
 
@@ -398,7 +406,7 @@ f8_product_few_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_con
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *tmem_slot;
+    const uint32_t tmem = (uint32_t)uniform((int)*tmem_slot);
     chained_wait();
 
     float acc[NT];
@@ -425,23 +433,21 @@ f8_product_few_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_con
             }
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            int stage = 0, buf = 0;
-            uint32_t phase = 0, acc_phase = 0;
-            for (int b = b0; b < b1; ++b) {
-                if (!mbar_wait_bounded(acc_empty(buf), acc_phase ^ 1u, abort_flag) ||
-                    !mbar_wait_bounded(full_bar(stage), phase, abort_flag))
-                    break;
-                tc_fence_after();
-                const uint32_t w = kF8DescLo + ((base + stage * F::stage_bytes) >> 4);
+        int stage = 0, buf = 0;
+        uint32_t phase = 0, acc_phase = 0;
+        for (int b = b0; b < b1; ++b) {
+            if (!__all_sync(0xffffffffu, mbar_wait_bounded(acc_empty(buf), acc_phase ^ 1u, abort_flag) &&
+                                             mbar_wait_bounded(full_bar(stage), phase, abort_flag)))
+                break;
+            tc_fence_after();
+            const uint32_t w = kF8DescLo + ((base + stage * F::stage_bytes) >> 4);
 #pragma unroll
-                for (int ks = 0; ks < 4; ++ks)
-                    tc_mma_f8(tmem + buf * NT, w + 2 * ks, w + 2 * ks + (128 * kF8Block >> 4), f8_idesc(NT), ks > 0);
-                tc_commit(empty_bar(stage));
-                tc_commit(acc_full(buf));
-                if (++stage == F::stages) { stage = 0; phase ^= 1u; }
-                if (++buf == F::bufs) { buf = 0; acc_phase ^= 1u; }
-            }
+            for (int ks = 0; ks < 4; ++ks)
+                tc_mma_f8(tmem + buf * NT, w + 2 * ks, w + 2 * ks + (128 * kF8Block >> 4), f8_idesc(NT), ks > 0);
+            tc_commit_elected(empty_bar(stage));
+            tc_commit_elected(acc_full(buf));
+            if (++stage == F::stages) { stage = 0; phase ^= 1u; }
+            if (++buf == F::bufs) { buf = 0; acc_phase ^= 1u; }
         }
     } else {
         const int quarter = warp & 3, t = threadIdx.x - 64;
