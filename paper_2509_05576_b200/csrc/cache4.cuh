@@ -14,6 +14,7 @@
 #include "common.cuh"
 #include "fp8.cuh"
 #include "tc.cuh"
+#include <type_traits>
 
 namespace ptq {
 
@@ -306,6 +307,9 @@ struct Attn4 {
     int32_t* status;
 };
 
+// What beginning and ending a row tile costs a warp, in chunks.
+constexpr int kFewTileCost = 1;
+
 struct AttnRows { int row0, n, len; };                   // rows row0 .. row0 + n - 1, the last of len tokens
 __device__ __forceinline__ AttnRows attn_rows(const Attn4& a, int b) {
     AttnRows r;
@@ -331,7 +335,7 @@ __device__ __forceinline__ AttnRequest attn_request(const Attn4& a, int b) {
     const int low = a.window > 0 ? (int)min(max((long long)r.len - r.n - a.window + 1, 0ll), (long long)r.len) : 0;
     r.chunk0 = low / kChunk;
     r.chunks = max((r.len + kChunk - 1) / kChunk - r.chunk0, 1);          // a request without keys still has rows to write
-    r.units = (long long)a.cache.kv_heads * r.tiles * r.chunks;
+    r.units = (long long)a.cache.kv_heads * r.tiles * (r.chunks + kFewTileCost);
     return r;
 }
 // Keys [lo, hi) that row token i of the request sees.
@@ -402,20 +406,19 @@ __device__ __forceinline__ float attn_lse(float ref, float sum, float shift) {
 template <typename T> constexpr bool kIsHalf = false;
 template <> constexpr bool kIsHalf<__half> = true;
 
-constexpr int kFewWarps = 8, kFewStages = 3, kFewMaxCtas = 320;
+constexpr int kFewWarps = 8, kFewStages = 3, kFewThreads = 32 * kFewWarps;
 template <int HD> struct FewShape {
     static constexpr int tiles = HD == 128 ? 2 : 4;                   // tiles of a chunk: 4608 bytes either way
     static constexpr int chunk = tiles * kC4Tile;
     static constexpr int chunk_bytes = tiles * c4_tile_bytes(HD);
-    static constexpr int ring_bytes = kFewWarps * kFewStages * chunk_bytes;
-    static constexpr int smem_bytes = ring_bytes + 1024;
+    static constexpr int smem_bytes = kFewWarps * kFewStages * chunk_bytes + 128;
 };
 __host__ __device__ constexpr int few_partial_floats(int hd, int nt) { return 8 * nt * (hd + 2); }
+constexpr int few_max_ctas(int nt) { return nt == 1 ? 320 : 160; }
 
-// The units of all requests are dealt to the CTAs in equal shares, in the order (request, kv head, row tile, chunk): a long request
-// and a batch of short ones fill the GPU alike.  A CTA finds its share by adding up the requests' units, 256 at a time.
-constexpr int kFewThreads = 32 * kFewWarps;
-struct FewScan { long long warp[kFewWarps]; long long before; int b; };
+// The units of all requests are dealt to the warps of the grid in equal shares, in the order (request, kv head, row tile, chunk): a
+// long request and a batch of short ones fill the GPU alike.  A warp finds its share by adding up the requests' units, 256 at a time.
+struct FewScan { long long warp[kFewWarps]; long long starts[kFewThreads]; };
 template <int kRows, int kChunk>
 __device__ __forceinline__ long long few_total(const Attn4& a, FewScan& s) {
     long long mine = 0;
@@ -430,129 +433,180 @@ __device__ __forceinline__ long long few_total(const Attn4& a, FewScan& s) {
     __syncthreads();
     return total;
 }
-// Sum of v over the threads before this one; `all`: over all of them.
-__device__ __forceinline__ long long few_scan(long long v, FewScan& s, long long& all) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    long long x = v;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const long long y = __shfl_up_sync(0xffffffffu, x, d);
-        if (lane >= d) x += y;
-    }
-    if (lane == 31) s.warp[warp] = x;
-    __syncthreads();
-    all = 0;
-    long long before = 0;
-#pragma unroll
-    for (int w = 0; w < kFewWarps; ++w) {
-        if (w == warp) before = all;
-        all += s.warp[w];
-    }
-    __syncthreads();
-    return before + x - v;
-}
-// The request that unit u belongs to (s.b) and the units before it (s.before); u < total.
+// The request that this warp's unit u belongs to and the units before it; all warps of the CTA, each with a u of its own (u >= total:
+// none).
 template <int kRows, int kChunk>
-__device__ __forceinline__ void few_find(const Attn4& a, long long u, FewScan& s) {
+__device__ __forceinline__ int few_find(const Attn4& a, long long u, FewScan& s, long long& before) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     long long base = 0;
-    for (int first = 0; first < a.batch && base <= u; first += kFewThreads) {
+    int found = -1;
+    for (int first = 0; first < a.batch; first += kFewThreads) {
         const int b = first + threadIdx.x;
         const long long mine = b < a.batch ? attn_request<kRows, kChunk>(a, b).units : 0;
-        long long all;
-        const long long before = base + few_scan(mine, s, all);
-        if (before <= u && u < before + mine) { s.b = b; s.before = before; }
+        long long x = mine;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const long long y = __shfl_up_sync(0xffffffffu, x, d);
+            if (lane >= d) x += y;
+        }
+        if (lane == 31) s.warp[warp] = x;
+        __syncthreads();
+        long long all = 0, at = 0;
+#pragma unroll
+        for (int w = 0; w < kFewWarps; ++w) {
+            if (w == warp) at = all;
+            all += s.warp[w];
+        }
+        s.starts[threadIdx.x] = base + at + x - mine;
+        __syncthreads();
+        if (base <= u && u < base + all) {               // the last request that starts at or before u
+            int count = 0;
+#pragma unroll
+            for (int i = 0; i < kFewThreads / 32; ++i) count += __popc(__ballot_sync(0xffffffffu, s.starts[i * 32 + lane] <= u));
+            found = first + count - 1;
+            before = s.starts[count - 1];
+        }
         base += all;
+        __syncthreads();
     }
-    __syncthreads();
+    return found;
 }
-__device__ __forceinline__ long long few_share(long long total, int ctas) {
-    const long long even = (total + ctas - 1) / ctas;
-    return even < kFewWarps ? kFewWarps : even;          // less than a chunk a warp would only add partial results
-}
+__device__ __forceinline__ long long few_share(long long total, int workers) { return total > workers ? (total + workers - 1) / workers : 1; }
 
-// Few rows (the new tokens of a request times the query heads of a kv head, up to 8 NT): what counts is one read of the cache.
-// A warp takes every eighth chunk of the CTA's share and keeps three of them in flight (bulk copies, 4608 bytes each; sixteen
-// warps an SM).  The cache is the 16-row operand of the tensor cores and the query rows their eight columns, so that a group of up to
-// eight query heads costs half of what it would the other way round:  S^T = K q (16 tokens x 8 rows), O^T = V^T P^T (16 values x
-// 8 rows).  Codes go from shared memory to registers as they lie and become fp16 there: three instructions for two values.
+// A warp's part of a row tile: chunks [from, to), counted from the request's first.
+struct FewPiece {
+    AttnRequest r;
+    int b, head, first_row, live_rows, from, to;
+    int lo_any, hi_any, lo_all, hi_all;                  // keys that any, and that every row of the tile sees
+    int c, c_end, last_tile;                             // its chunks that hold such keys, the end of its 16-token tiles
+};
+template <int kRows, int kChunk>
+struct FewWalk {
+    long long u, end, before;
+    int b;
+    __device__ __forceinline__ bool next(const Attn4& a, FewPiece& p) {
+        while (u < end) {
+            p.r = attn_request<kRows, kChunk>(a, b);
+            if (u >= before + p.r.units) { before += p.r.units; ++b; continue; }
+            const int length = p.r.chunks + kFewTileCost, seg = (int)((u - before) / length), x0 = (int)((u - before) - (long long)seg * length);
+            const int x1 = (int)min((long long)length, x0 + (end - u));
+            u += x1 - x0;
+            p.from = max(x0 - kFewTileCost, 0);
+            p.to = x1 - kFewTileCost;
+            if (p.to <= p.from) continue;                // only what stands for the tile's beginning
+            p.b = b;
+            p.head = seg / p.r.tiles;
+            p.first_row = (seg - p.head * p.r.tiles) * kRows;
+            p.live_rows = min(kRows, p.r.rows - p.first_row);
+            attn_range(a, p.r, p.first_row / a.ratio, p.lo_any, p.hi_all);
+            attn_range(a, p.r, (p.first_row + p.live_rows - 1) / a.ratio, p.lo_all, p.hi_any);
+            p.c = max(p.r.chunk0 + p.from, p.lo_any / kChunk);
+            p.c_end = min(p.r.chunk0 + p.to, (p.hi_any + kChunk - 1) / kChunk);
+            p.last_tile = (p.hi_any + kC4Tile - 1) / kC4Tile;
+            return true;
+        }
+        return false;
+    }
+};
+
+// Few rows (the new tokens of a request times the query heads of a kv head, up to 8 NT at a time): what counts is one read of the cache.
+// Every warp works by itself, with three chunks in flight (bulk copies of 2304 bytes, sixteen warps an SM); a row tile that lies in
+// one warp's share is finished by it, others are joined afterwards.
+// The cache is the 16-row operand of the tensor cores and the query rows their eight columns, so that a group of up to eight query
+// heads costs half of what it would the other way round:  S^T = K q (16 tokens x 8 rows), O^T = V^T P^T (16 values x 8 rows).
+// Codes go from shared memory to registers as they lie and become fp16 there: three instructions for two values.
 // The order of a contraction is free, so the four lanes that share a token take 32 consecutive values each, and q is laid out alike.
 template <typename T, int HD, int NT>
 __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) attn4_few_kernel(Attn4 a) {
     using F = FewShape<HD>;
-    constexpr int kRows = 8 * NT, kWords = HD / 32, kSteps = HD / 16, kTiles = HD / 16;
+    constexpr int kRows = 8 * NT, kWords = HD / 32, kSteps = HD / 16, kTiles = HD / 16, kLane = HD / 8;
     constexpr int kSide = c4_side_bytes(HD), kTileBytes = c4_tile_bytes(HD), kCodes = kC4Tile * HD / 2, kGrids = HD / kC4Group * 2;
     extern __shared__ unsigned char few_smem_raw[];
     __shared__ FewScan scan;
     __shared__ uint64_t bars[kFewWarps * kFewStages];
-    __shared__ float stat_m[kFewWarps][kRows], stat_l[kFewWarps][kRows];
     __shared__ int abort_word;
-    unsigned char* ring = few_smem_raw + (1024 - (smem_u32(few_smem_raw) & 1023)) % 1024;
+    unsigned char* ring = few_smem_raw + (128 - (smem_u32(few_smem_raw) & 127)) % 128;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n8 = lane >> 2, t = lane & 3;
-    const uint32_t ring_w = smem_u32(ring) + warp * kFewStages * F::chunk_bytes;
     const unsigned char* ring_p = ring + warp * kFewStages * F::chunk_bytes;
-    const uint32_t bar_w = smem_u32(&bars[warp * kFewStages]);
+    const uint32_t ring_w = smem_u32(ring_p), bar_w = smem_u32(&bars[warp * kFewStages]);
     if (lane < kFewStages) mbar_init(bar_w + 8 * lane, 1);
-    if (threadIdx.x == 0) { scan.b = 0; scan.before = 0; abort_word = 0; }
+    if (threadIdx.x == 0) abort_word = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncthreads();
     chained_begin();
 
-    const long long total = few_total<kRows, F::chunk>(a, scan), share = few_share(total, gridDim.x);
-    long long u = share * blockIdx.x;
-    const long long u_end = min(u + share, total);
-    if (u >= total) return;
-    few_find<kRows, F::chunk>(a, u, scan);
-    int b = scan.b;
-    long long before = scan.before;
-    unsigned uses = 0;                                   // chunks this warp has asked for so far, over all pieces
-    unsigned done = 0;
+    // workers side by side lie on different SMs: a small problem then uses as many of them as it has chunks
+    const int worker = warp * gridDim.x + blockIdx.x, workers = kFewWarps * gridDim.x;
+    const long long total = few_total<kRows, F::chunk>(a, scan), share = few_share(total, workers);
+    FewWalk<kRows, F::chunk> walk;
+    walk.u = share * worker;
+    walk.end = min(walk.u + share, total);
+    walk.before = 0;
+    walk.b = few_find<kRows, F::chunk>(a, walk.u, scan, walk.before);
 
-    while (u < u_end) {
-        AttnRequest r = attn_request<kRows, F::chunk>(a, b);
-        while (u >= before + r.units) { before += r.units; ++b; r = attn_request<kRows, F::chunk>(a, b); }
-        const int seg = (int)((u - before) / r.chunks), from = (int)((u - before) - (long long)seg * r.chunks);
-        const int head = seg / r.tiles, tile = seg - head * r.tiles;
-        const int to = (int)min((long long)r.chunks, from + (u_end - u));
-        u += to - from;
-        const int first_row = tile * kRows, live_rows = min(kRows, r.rows - first_row);
-        // keys that any row, and that every row of the tile sees
-        int lo_any, hi_any, lo_all, hi_all;
-        attn_range(a, r, first_row / a.ratio, lo_any, hi_all);           // rows that do not exist may compute anything: nobody reads them
-        attn_range(a, r, (first_row + live_rows - 1) / a.ratio, lo_all, hi_any);
-        const int c_first = max(r.chunk0 + from, lo_any / F::chunk), c_last = min(r.chunk0 + to, (hi_any + F::chunk - 1) / F::chunk);
-
+    unsigned asked = 0, done = 0;                        // chunks so far, over all pieces
+    FewPiece p;
+    int next = 0;
+    auto ask = [&]() {                                   // the next chunk's tiles that hold keys; the whole warp
+        const int stage = asked % kFewStages, tile0 = next * F::tiles, count = min(F::tiles, p.last_tile - tile0);
+        const uint32_t bar = bar_w + 8 * stage;
+        if (lane == 0) mbar_arrive_expect_tx(bar, count * kTileBytes);
+        __syncwarp();
+        if (lane < count) {
+            const int tl = tile0 + lane, per = a.cache.page_shift - 4;
+            int page = a.table[(int64_t)p.b * a.ldt + (tl >> per)];
+            if (page < 0 || page >= a.cache.num_pages) { report(a.status, PTQ_ERR_INVALID_ARG, p.b, 2); page = 0; }
+            bulk_load(ring_w + stage * F::chunk_bytes + lane * kTileBytes, c4_tile<HD>(a.cache, page, p.head, tl & ((1 << per) - 1)), kTileBytes, bar);
+        }
+        ++asked;
+        ++next;
+    };
+    auto begin = [&]() {
+        next = p.c;
+#pragma unroll
+        for (int s = 0; s < kFewStages; ++s)
+            if (next < p.c_end) ask();
+    };
+    bool more = walk.next(a, p), ok = true;
+    if (more) begin();
+    while (more && ok) {
         // the query rows, in the order in which the codes come
         uint32_t qf[NT][kSteps][2];
         float mult[NT][2];
         int lo[NT][2], hi[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const int row = first_row + nt * 8 + n8;
-            float v[8 * kWords], top = 0.f;
-            const bool live = row < r.rows;
+            const int row = p.first_row + nt * 8 + n8;
+            const bool live = row < p.r.rows;
             const int i = live ? row / a.ratio : 0;
-            const T* q = static_cast<const T*>(a.q) + (int64_t)(r.row0 + i) * a.q_token + (int64_t)(head * a.ratio + (live ? row - i * a.ratio : 0)) * a.q_head;
+            const T* q = static_cast<const T*>(a.q) + (int64_t)(p.r.row0 + i) * a.q_token + (int64_t)(p.head * a.ratio + (live ? row - i * a.ratio : 0)) * a.q_head;
+            float v[kWords][8], top = 0.f;
+            bool bad = false;
 #pragma unroll
-            for (int j = 0; j < 8 * kWords; ++j) { v[j] = live ? to_f32<T>(q[t * 8 * kWords + j]) : 0.f; top = fmaxf(top, fabsf(v[j])); if (not_finite(v[j])) top = __uint_as_float(0x7f800000u); }
+            for (int w = 0; w < kWords; ++w) load8<T>(q + (t * kWords + w) * 8, live ? 8 : 0, a.q_vec, v[w]);
+#pragma unroll
+            for (int w = 0; w < kWords; ++w)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) { top = fmaxf(top, fabsf(v[w][e])); bad |= not_finite(v[w][e]); }
+            if (bad) top = __uint_as_float(0x7f800000u);
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            const int shift = sizeof(T) == 2 && !kIsHalf<T> ? attn_q_shift(top) : 0;
+            const int shift = kIsHalf<T> ? 0 : attn_q_shift(top);
             const float f = exp2_int(shift);
 #pragma unroll
             for (int w = 0; w < kWords; ++w)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const float* x = v + 8 * w + 2 * h;
-                    qf[nt][2 * w + h][0] = pack_half2(x[0] * f, x[4] * f);
-                    qf[nt][2 * w + h][1] = pack_half2(x[1] * f, x[5] * f);
+                    qf[nt][2 * w + h][0] = pack_half2(v[w][2 * h] * f, v[w][2 * h + 4] * f);
+                    qf[nt][2 * w + h][1] = pack_half2(v[w][2 * h + 1] * f, v[w][2 * h + 5] * f);
                 }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int rr = first_row + nt * 8 + 2 * t + h;
+                const int rr = p.first_row + nt * 8 + 2 * t + h;
                 mult[nt][h] = a.scale_log2 * exp2_int(-__shfl_sync(0xffffffffu, shift, (2 * t + h) * 4));
                 lo[nt][h] = hi[nt][h] = 0;
-                if (rr < r.rows) attn_range(a, r, rr / a.ratio, lo[nt][h], hi[nt][h]);
+                if (rr < p.r.rows) attn_range(a, p.r, rr / a.ratio, lo[nt][h], hi[nt][h]);
             }
         }
 
@@ -566,33 +620,9 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) attn4_few_kernel
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[nt][j][e] = 0.f;
         }
-        const int last_tile = (hi_any + kC4Tile - 1) / kC4Tile;
-        auto ask = [&](int c) {                          // the tiles of chunk c that hold keys; the whole warp
-            const int stage = uses % kFewStages, tile0 = c * F::tiles, count = min(F::tiles, last_tile - tile0);
-            const uint32_t bar = bar_w + 8 * stage;
-            if (lane == 0) mbar_arrive_expect_tx(bar, count * kTileBytes);
-            __syncwarp();
-            if (lane < count) {
-                const int tl = tile0 + lane, per = a.cache.page_shift - 4;
-                int page = a.table[(int64_t)b * a.ldt + (tl >> per)];
-                if (page < 0 || page >= a.cache.num_pages) { report(a.status, PTQ_ERR_INVALID_ARG, b, 2); page = 0; }
-                bulk_load(ring_w + stage * F::chunk_bytes + lane * kTileBytes, c4_tile<HD>(a.cache, page, head, tl & ((1 << per) - 1)), kTileBytes, bar);
-            }
-            ++uses;
-        };
-        int next = c_first + warp;
-#pragma unroll
-        for (int s = 0; s < kFewStages; ++s)
-            if (next < c_last) { ask(next); next += kFewWarps; }
-        bool ok = true;
-        for (int c = c_first + warp; c < c_last; c += kFewWarps) {
-            const int stage = done % kFewStages;
-            ok = __all_sync(0xffffffffu, mbar_wait_bounded(bar_w + 8 * stage, (done / kFewStages) & 1, &abort_word));
-            if (!ok) break;
-            ++done;
-            const unsigned char* data = ring_p + stage * F::chunk_bytes;
-            const int j0 = c * F::chunk;
-            const bool whole = j0 >= lo_all && j0 + F::chunk <= hi_all;
+        // one chunk; `masked`: some row does not see all of it
+        auto chunk = [&](const unsigned char* data, int j0, auto masked) {
+            constexpr bool kMasked = decltype(masked)::value;
             float x[NT][F::tiles][4];
 #pragma unroll
             for (int tl = 0; tl < F::tiles; ++tl) {
@@ -605,7 +635,7 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) attn4_few_kernel
                     if constexpr (HD == 128) *reinterpret_cast<uint4*>(kw[h]) = *reinterpret_cast<const uint4*>(side + token * (HD / 2) + t * 16);
                     else *reinterpret_cast<uint2*>(kw[h]) = *reinterpret_cast<const uint2*>(side + token * (HD / 2) + t * 8);
                     const uint32_t g = *reinterpret_cast<const uint16_t*>(side + kCodes + token * kGrids + t * 8 * kWords / kC4Group * 2);
-                    f[h] = c4_factors(g | g << 16);
+                    f[h] = c4_factors(__byte_perm(g, g, 0x1010));
                 }
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
@@ -632,7 +662,7 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) attn4_few_kernel
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         float v = x[nt][tl][e] * mult[nt][e & 1];
-                        if (!whole) {
+                        if (kMasked) {
                             const int j = j0 + tl * kC4Tile + n8 + 8 * (e >> 1);
                             if (j < lo[nt][e & 1] || j >= hi[nt][e & 1]) v = -INFINITY;
                         }
@@ -686,12 +716,12 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) attn4_few_kernel
                     if constexpr (HD == 128) *reinterpret_cast<uint2*>(vw[e]) = *reinterpret_cast<const uint2*>(side + token * (HD / 2) + n8 * 8);
                     else vw[e][0] = *reinterpret_cast<const uint32_t*>(side + token * (HD / 2) + n8 * 4);
                     g[e] = *reinterpret_cast<const uint16_t*>(side + kCodes + token * kGrids + n8 * 8 * kV / kC4Group * 2);
-                    if (!whole) {                                 // what nobody sees may hold anything: 0 times it has to be 0
+                    if (kMasked) {                                // what nobody sees may hold anything: 0 times it has to be 0
                         const int j = j0 + tl * kC4Tile + token;
-                        if (j < lo_any || j >= hi_any) g[e] = 0u;
+                        if (j < p.lo_any || j >= p.hi_any) g[e] = 0u;
                     }
                 }
-                const C4Factors f0 = c4_factors(g[0] | g[1] << 16), f1 = c4_factors(g[2] | g[3] << 16);
+                const C4Factors f0 = c4_factors(__byte_perm(g[0], g[1], 0x5410)), f1 = c4_factors(__byte_perm(g[2], g[3], 0x5410));
 #pragma unroll
                 for (int w = 0; w < kV; ++w)
 #pragma unroll
@@ -706,102 +736,141 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) attn4_few_kernel
                                 mma_f16(o[nt][4 * w + 2 * h + e], v0[2 * e], v0[2 * e + 1], v1[2 * e], v1[2 * e + 1], pf[nt][tl][0], pf[nt][tl][1]);
                     }
             }
+        };
+        for (int c = p.c; c < p.c_end; ++c) {
+            const int stage = done % kFewStages, j0 = c * F::chunk;
+            ok = __all_sync(0xffffffffu, mbar_wait_bounded(bar_w + 8 * stage, (done / kFewStages) & 1, &abort_word));
+            if (!ok) break;
+            ++done;
+            if (j0 >= p.lo_all && j0 + F::chunk <= p.hi_all) chunk(ring_p + stage * F::chunk_bytes, j0, std::false_type());
+            else chunk(ring_p + stage * F::chunk_bytes, j0, std::true_type());
             __syncwarp();                                         // the stage has been read
-            if (next < c_last) { ask(next); next += kFewWarps; }
+            if (next < p.c_end) ask();
         }
-        if (!ok) {                                                // copies in flight land before the ring is reused or left
-            for (; done < uses; ++done) drain_copy(bar_w + 8 * (done % kFewStages), (done / kFewStages) & 1);
+        if (!ok) {                                                // copies in flight land before the CTA is left
+            for (; done < asked; ++done) drain_copy(bar_w + 8 * (done % kFewStages), (done / kFewStages) & 1);
             if (lane == 0) report(a.status, PTQ_ERR_TIMEOUT, blockIdx.x, 3);
+            break;
         }
-
-        // the warps' results become one, through the ring: [warp][row][value]
-        __syncthreads();
-        float* joint = reinterpret_cast<float*>(ring);
+        // the next piece's first chunks are under way while this one's results are written
+        const FewPiece old = p;
+        more = walk.next(a, p);
+        if (more) begin();
+        const bool complete = old.from == 0 && old.to == old.r.chunks;
+        float* slot = a.partial + (int64_t)(2 * worker + (old.from == 0 ? 1 : 0)) * few_partial_floats(HD, NT);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
 #pragma unroll
                 for (int d = 4; d < 32; d <<= 1) l[nt][h] += __shfl_xor_sync(0xffffffffu, l[nt][h], d);
-                const int row = nt * 8 + 2 * t + h;
-                if (n8 == 0) { stat_m[warp][row] = m[nt][h]; stat_l[warp][row] = l[nt][h]; }
-                float* dst = joint + (warp * kRows + row) * HD + n8 * (HD / 8);
+                const int in = nt * 8 + 2 * t + h;
+                if (in >= old.live_rows) continue;
+                float v[kLane];
+                if (complete) {
+                    const float inv = l[nt][h] == 0.f ? 0.f : 1.f / l[nt][h];
 #pragma unroll
-                for (int j = 0; j < kTiles; ++j) *reinterpret_cast<float2*>(dst + 2 * j) = make_float2(o[nt][j][h], o[nt][j][h + 2]);
-            }
-        __syncthreads();
-        const bool complete = from == 0 && to == r.chunks;
-        float* slot = a.partial + (int64_t)(2 * blockIdx.x + (from == 0 ? 1 : 0)) * few_partial_floats(HD, NT);
-        for (int e = threadIdx.x; e < live_rows * (HD / 2); e += kFewThreads) {
-            const int row = e / (HD / 2), d = e % (HD / 2) * 2;
-            float top = -INFINITY, sum = 0.f, v0 = 0.f, v1 = 0.f;
+                    for (int j = 0; j < kTiles; ++j) { v[2 * j] = o[nt][j][h] * inv; v[2 * j + 1] = o[nt][j][h + 2] * inv; }
+                    const int rr = old.first_row + in, i = rr / a.ratio, qh = old.head * a.ratio + rr - i * a.ratio;
+                    store_row<T, kLane>(static_cast<T*>(a.out) + (int64_t)(old.r.row0 + i) * a.o_token + (int64_t)qh * a.o_head + n8 * kLane, v, a.o_vec);
+                    if (n8 == 0 && a.lse)
+                        a.lse[(int64_t)(old.r.row0 + i) * a.q_heads + qh] = attn_lse(m[nt][h] == -INFINITY ? 0.f : m[nt][h], l[nt][h], kAttnPShift);
+                } else {
 #pragma unroll
-            for (int w = 0; w < kFewWarps; ++w) top = fmaxf(top, stat_m[w][row]);
-            const float ref = top == -INFINITY ? 0.f : top;
-#pragma unroll
-            for (int w = 0; w < kFewWarps; ++w) {
-                const float f = exp2_approx(stat_m[w][row] - ref);
-                const float2 v = *reinterpret_cast<const float2*>(joint + (w * kRows + row) * HD + d);
-                sum += f * stat_l[w][row];
-                v0 += f * v.x;
-                v1 += f * v.y;
+                    for (int j = 0; j < kTiles; ++j) { v[2 * j] = o[nt][j][h]; v[2 * j + 1] = o[nt][j][h + 2]; }
+                    store_row<float, kLane>(slot + in * HD + n8 * kLane, v, true);
+                    if (n8 == 0) { slot[kRows * HD + in] = m[nt][h]; slot[kRows * (HD + 1) + in] = l[nt][h]; }
+                }
             }
-            if (complete) {
-                const int rr = first_row + row, i = rr / a.ratio, qh = head * a.ratio + rr - i * a.ratio;
-                const float inv = sum == 0.f ? 0.f : 1.f / sum;
-                T* out = static_cast<T*>(a.out) + (int64_t)(r.row0 + i) * a.o_token + (int64_t)qh * a.o_head + d;
-                out[0] = from_f32<T>(v0 * inv);
-                out[1] = from_f32<T>(v1 * inv);
-                if (d == 0 && a.lse) a.lse[(int64_t)(r.row0 + i) * a.q_heads + qh] = attn_lse(ref, sum, kAttnPShift);
-            } else {
-                *reinterpret_cast<float2*>(slot + row * HD + d) = make_float2(v0, v1);
-                if (d == 0) { slot[kRows * HD + row] = top; slot[kRows * (HD + 1) + row] = sum; }
-            }
-        }
-        __syncthreads();
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the ring is written by copies again
-        if (abort_word) return;
     }
 }
 
-// Joins the partial results of what several CTAs share: CTA c looks at the border between the shares of c and c + 1, and if that is
-// the first border inside a row tile, adds up the tile's pieces in their order, a warp a row.
+// Joins the partial results of row tiles that several warps shared.  Warp w of CTA c looks at the border behind worker
+// c 8 + w: if it is the first one inside a tile, the CTA adds up that tile's pieces, in their order: a warp a row, or, where
+// the pieces are many, all warps a row together, each an eighth of the pieces.
+constexpr int kJoinTogether = 16;
 template <typename T, int HD, int NT>
 __global__ void __launch_bounds__(kFewThreads) attn4_join_kernel(Attn4 a, int ctas) {
     using F = FewShape<HD>;
     constexpr int kRows = 8 * NT, kLane = HD / 32;
     __shared__ FewScan scan;
+    struct Job { int b, head, tile, w0, w1; };
+    __shared__ Job jobs[kFewWarps];
+    __shared__ float part_top[kFewWarps], part_sum[kFewWarps], part_v[kFewWarps][HD];
     chained_begin();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const long long total = few_total<kRows, F::chunk>(a, scan), share = few_share(total, ctas), u = share * (blockIdx.x + 1);
-    if (u >= total) return;
-    few_find<kRows, F::chunk>(a, u, scan);
-    const AttnRequest r = attn_request<kRows, F::chunk>(a, scan.b);
-    const int seg = (int)((u - scan.before) / r.chunks), head = seg / r.tiles, tile = seg - head * r.tiles;
-    const long long s0 = scan.before + (long long)seg * r.chunks, s1 = s0 + r.chunks - 1;
-    if (s0 == u) return;                                          // a tile begins here
-    const int c0 = (int)(s0 / share), c1 = (int)(s1 / share);
-    if (c0 != (int)blockIdx.x) return;                            // an earlier border is the tile's first
-    const int first_row = tile * kRows, live_rows = min(kRows, r.rows - first_row);
-    for (int row = warp; row < live_rows; row += kFewWarps) {
-        float top = -INFINITY, sum = 0.f, v[kLane];
-#pragma unroll
-        for (int i = 0; i < kLane; ++i) v[i] = 0.f;
-        for (int c = c0; c <= c1; ++c) top = fmaxf(top, a.partial[(int64_t)(2 * c + (c == c0)) * few_partial_floats(HD, NT) + kRows * HD + row]);
-        const float ref = top == -INFINITY ? 0.f : top;
-        for (int c = c0; c <= c1; ++c) {
-            const float* slot = a.partial + (int64_t)(2 * c + (c == c0)) * few_partial_floats(HD, NT);
-            const float f = exp2_approx(slot[kRows * HD + row] - ref);
-            sum += f * slot[kRows * (HD + 1) + row];
-#pragma unroll
-            for (int i = 0; i < kLane; ++i) v[i] += f * slot[row * HD + lane * kLane + i];
-        }
-        const int rr = first_row + row, i0 = rr / a.ratio, qh = head * a.ratio + rr - i0 * a.ratio;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, workers = ctas * kFewWarps, border = blockIdx.x * kFewWarps + warp;
+    const long long total = few_total<kRows, F::chunk>(a, scan), share = few_share(total, workers), u = share * (border + 1);
+    if (share * (blockIdx.x * kFewWarps + 1) >= total) return;
+    long long before = 0;
+    const int b = few_find<kRows, F::chunk>(a, u, scan, before);
+    Job mine{-1, 0, 0, 0, 0};
+    if (b >= 0) {
+        const AttnRequest r = attn_request<kRows, F::chunk>(a, b);
+        const int length = r.chunks + kFewTileCost, seg = (int)((u - before) / length);
+        const long long s0 = before + (long long)seg * length + kFewTileCost;          // its first chunk
+        const long long w0 = s0 / share, w1 = (s0 + r.chunks - 1) / share;
+        if (u > s0 && w0 == border) mine = Job{b, seg / r.tiles, seg % r.tiles, (int)w0, (int)w1};
+    }
+    if (lane == 0) jobs[warp] = mine;
+    __syncthreads();
+    auto weight = [&](int w, int w0, int row) -> const float* {
+        return a.partial + (int64_t)(2 * w + (w == w0)) * few_partial_floats(HD, NT) + kRows * HD + row;
+    };
+    auto finish = [&](const AttnRequest& r, const Job& j, int row, float ref, float sum, const float (&v)[kLane]) {
+        const int rr = j.tile * kRows + row, i0 = rr / a.ratio, qh = j.head * a.ratio + rr - i0 * a.ratio;
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
         T* out = static_cast<T*>(a.out) + (int64_t)(r.row0 + i0) * a.o_token + (int64_t)qh * a.o_head + lane * kLane;
 #pragma unroll
         for (int i = 0; i < kLane; ++i) out[i] = from_f32<T>(v[i] * inv);
         if (lane == 0 && a.lse) a.lse[(int64_t)(r.row0 + i0) * a.q_heads + qh] = attn_lse(ref, sum, kAttnPShift);
+    };
+    for (int k = 0; k < kFewWarps; ++k) {
+        const Job j = jobs[k];
+        if (j.b < 0) continue;
+        const AttnRequest r = attn_request<kRows, F::chunk>(a, j.b);
+        const int live_rows = min(kRows, r.rows - j.tile * kRows);
+        const bool together = j.w1 - j.w0 >= kJoinTogether;
+        for (int row = together ? 0 : warp; row < live_rows; row += together ? 1 : kFewWarps) {
+            const int step = together ? kFewWarps : 1, w_first = j.w0 + (together ? warp : 0);
+            float top = -INFINITY, sum = 0.f, v[kLane];
+#pragma unroll
+            for (int i = 0; i < kLane; ++i) v[i] = 0.f;
+            for (int w = w_first + lane * step; w <= j.w1; w += 32 * step) top = fmaxf(top, *weight(w, j.w0, row));
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+            const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll 4
+            for (int w = w_first; w <= j.w1; w += step) {
+                const float* stat = weight(w, j.w0, row);
+                const float f = exp2_approx(stat[0] - ref);
+                sum += f * stat[kRows];
+#pragma unroll
+                for (int i = 0; i < kLane; ++i) v[i] += f * stat[row * HD - kRows * HD - row + lane * kLane + i];
+            }
+            if (!together) {
+                finish(r, j, row, ref, sum, v);
+                continue;
+            }
+            if (lane == 0) { part_top[warp] = top; part_sum[warp] = sum; }
+#pragma unroll
+            for (int i = 0; i < kLane; ++i) part_v[warp][lane * kLane + i] = v[i];
+            __syncthreads();
+            if (warp == 0) {
+                float all_top = -INFINITY, all = 0.f, w[kLane];
+                for (int q = 0; q < kFewWarps; ++q) all_top = fmaxf(all_top, part_top[q]);
+                const float all_ref = all_top == -INFINITY ? 0.f : all_top;
+#pragma unroll
+                for (int i = 0; i < kLane; ++i) w[i] = 0.f;
+                for (int q = 0; q < kFewWarps; ++q) {
+                    const float f = exp2_approx(part_top[q] - all_ref);
+                    all += f * part_sum[q];
+#pragma unroll
+                    for (int i = 0; i < kLane; ++i) w[i] += f * part_v[q][lane * kLane + i];
+                }
+                finish(r, j, row, all_ref, all, w);
+            }
+            __syncthreads();
+        }
     }
 }
 

@@ -193,14 +193,24 @@ struct F8Product {
     int32_t* status;
 };
 
+// N consecutive values, in 16-byte pieces where vec says that they begin on 16 bytes.
+template <typename T, int N>
+__device__ __forceinline__ void store_row(T* p, const float* v, bool vec) {
+    if (vec) {
+        alignas(16) T t[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) t[i] = from_f32<T>(v[i]);
+#pragma unroll
+        for (int i = 0; i < N * (int)sizeof(T) / 16; ++i) reinterpret_cast<uint4*>(p)[i] = reinterpret_cast<const uint4*>(t)[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) p[i] = from_f32<T>(v[i]);
+    }
+}
 template <typename T>
-__device__ __forceinline__ void store_row16(T* p, const float* v, int n, bool vec) {      // sixteen consecutive outputs
-    if (vec && n >= 16) {
-        alignas(16) T t[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) t[i] = from_f32<T>(v[i]);
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(T); ++i) reinterpret_cast<uint4*>(p)[i] = reinterpret_cast<const uint4*>(t)[i];
+__device__ __forceinline__ void store_row16(T* p, const float* v, int n, bool vec) {      // sixteen of which n exist
+    if (n >= 16) {
+        store_row<T, 16>(p, v, vec);
     } else {
 #pragma unroll
         for (int i = 0; i < 16; ++i)

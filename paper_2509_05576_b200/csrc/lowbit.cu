@@ -144,14 +144,14 @@ cudaError_t allow_attn_smem_all() {
 
 template <typename T, int HD, int NT>
 void attn_few_launch(const Attn4& a, int sms, cudaStream_t stream) {
-    const int want = sms * (NT == 1 ? 2 : 1), ctas = want < kFewMaxCtas ? want : kFewMaxCtas;
+    const int want = sms * (NT == 1 ? 2 : 1), ctas = want < few_max_ctas(NT) ? want : few_max_ctas(NT);
     {
         Launch l(K_CACHE_ATTN_FEW, stream);
         launch_chained(attn4_few_kernel<T, HD, NT>, ctas, kFewThreads, FewShape<HD>::smem_bytes, stream, a);
     }
     {
         Launch l(K_CACHE_ATTN_JOIN, stream);
-        launch_chained(attn4_join_kernel<T, HD, NT>, ctas - 1, kFewThreads, 0, stream, a, ctas);
+        launch_chained(attn4_join_kernel<T, HD, NT>, ctas, kFewThreads, 0, stream, a, ctas);
     }
 }
 template <typename T, int HD>
@@ -184,7 +184,8 @@ AttnSpace attn_space(void* ws, int ratio, int head_dim, int batch, int total_q, 
     AttnSpace s{};
     Carver cv(ws);
     const int64_t rows = (int64_t)max_q * ratio;
-    s.few = cv.take<float>((size_t)2 * kFewMaxCtas * few_partial_floats(head_dim, rows <= 8 ? 1 : 2));
+    const int nt = rows <= 8 ? 1 : 2;
+    s.few = cv.take<float>((size_t)2 * few_max_ctas(nt) * kFewWarps * few_partial_floats(head_dim, nt));
     if (rows > kFewRows) {
         s.tiles = cv.take<float>((size_t)2 * kTileMaxCtas * tile_partial_floats(head_dim));
         s.list.most = (int)((int64_t)total_q * ratio / kTileRows) + batch;           // a last, partly filled tile for each request
