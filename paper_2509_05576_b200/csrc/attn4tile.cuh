@@ -19,6 +19,8 @@
 namespace ptq {
 
 constexpr int kTileRows = 256, kTileKeys = 128, kTileThreads = 512, kTileMaxCtas = 160, kScheduleThreads = 1024;
+// What beginning and ending a tile costs a CTA, in chunks.
+constexpr int kTileCost = 1;
 constexpr float kTilePShift = 8.f, kTileSlack = 7.f;     // P = 2^(x - ref + 8) <= 2^15
 
 template <int HD> struct TileShape {
@@ -75,7 +77,7 @@ __global__ void __launch_bounds__(kScheduleThreads) attn4_schedule_kernel(Attn4 
                 }
                 b = b0 + lo;
                 tile = f - first_tile[lo];
-                chunks = tile_range(a, attn_rows(a, b), tile).chunks;
+                chunks = tile_range(a, attn_rows(a, b), tile).chunks + kTileCost;
             }
             const longlong2 at = plan_scan(make_longlong2(chunks, 0), warp_sums, all);
             if (f < tiles && count + f < list.most) {
@@ -96,7 +98,7 @@ __global__ void __launch_bounds__(kScheduleThreads) attn4_schedule_kernel(Attn4 
 
 // A CTA's way through its share of the units.
 struct TilePiece {
-    int f, b, tile, head, from, to;      // chunks [from, to) of the tile, counted from its first
+    int b, tile, head, from, to;         // chunks [from, to) of the tile, counted from its first
     AttnRows r;
     TileRange range;
 };
@@ -104,21 +106,24 @@ struct TileWalk {
     long long u, end, share;
     int f;
     __device__ __forceinline__ bool next(const Attn4& a, const TileList& list, TilePiece& p) {
-        if (u >= end) return false;
         const long long heads = a.cache.kv_heads;
-        while (u >= heads * list.before[f + 1]) ++f;
-        const long long base = list.before[f], chunks = list.before[f + 1] - base, rel = u - heads * base;
-        p.f = f;
-        p.head = (int)(rel / chunks);
-        p.from = (int)(rel - p.head * chunks);
-        p.to = (int)min(chunks, p.from + (end - u));
-        const int2 t = list.tile[f];
-        p.b = t.x;
-        p.tile = t.y;
-        p.r = attn_rows(a, p.b);
-        p.range = tile_range(a, p.r, p.tile);
-        u += p.to - p.from;
-        return true;
+        while (u < end) {
+            while (u >= heads * list.before[f + 1]) ++f;
+            const long long base = list.before[f], length = list.before[f + 1] - base, rel = u - heads * base;
+            p.head = (int)(rel / length);
+            const int x0 = (int)(rel - p.head * length), x1 = (int)min(length, x0 + (end - u));
+            u += x1 - x0;
+            p.from = max(x0 - kTileCost, 0);
+            p.to = x1 - kTileCost;
+            if (p.to <= p.from) continue;                // only what stands for the tile's beginning
+            const int2 t = list.tile[f];
+            p.b = t.x;
+            p.tile = t.y;
+            p.r = attn_rows(a, p.b);
+            p.range = tile_range(a, p.r, p.tile);
+            return true;
+        }
+        return false;
     }
 };
 __device__ __forceinline__ long long tile_share(long long total, int ctas) { return (total + ctas - 1) / ctas; }
@@ -308,9 +313,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn4_tile_kernel(Attn4 a, Ti
                     for (int e = 0; e < 8; ++e) { top = fmaxf(top, fabsf(v[e])); bad |= not_finite(v[e]); }
                 }
                 const int shift = kIsHalf<T> || bad ? 0 : attn_q_shift(top);
-                // a negative scale changes the sign of q, a scale of 0 makes it 0: the factor of the scores is positive
-                const float f = (a.scale_log2 < 0.f ? -1.f : a.scale_log2 == 0.f ? 0.f : 1.f) * exp2_int(shift);
-                mult = a.scale_log2 == 0.f ? 1.f : fabsf(a.scale_log2) * exp2_int(-shift);
+                const float f = attn_q_sign(a.scale_log2) * exp2_int(shift);
+                mult = attn_score_factor(a.scale_log2, shift);
                 for (int c = 0; c < HD / 8; ++c) {
                     float v[8];
                     load8<T>(q + 8 * c, live ? 8 : 0, a.q_vec, v);
@@ -428,7 +432,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn4_tile_kernel(Attn4 a, Ti
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     uint32_t o[4];
-                    c4_unpack4(kw[4 * g + e], f, o);
+                    c4_unpack4(kw[4 * g + e], f, a.by, o);
                     *reinterpret_cast<uint4*>(stage + tile_at(kTileKeys, u, 4 * g + e)) = make_uint4(o[0], o[1], o[2], o[3]);
                 }
             }
@@ -442,7 +446,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn4_tile_kernel(Attn4 a, Ti
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         uint32_t o[4];
-                        c4_unpack4(__byte_perm(va[e], vb[e], h ? 0x7632 : 0x5410), f, o);
+                        c4_unpack4(__byte_perm(va[e], vb[e], h ? 0x7632 : 0x5410), f, a.by, o);
 #pragma unroll
                         for (int d = 0; d < 4; ++d) {
                             const int dim = dims * (HD / 2) + g * 32 + e * 8 + h * 4 + d;
@@ -546,11 +550,11 @@ __global__ void __launch_bounds__(256) attn4_tile_join_kernel(Attn4 a, TileList 
     if (u >= total) return;
     tile_find(a, list, count, u, &found);
     const int f = found;
-    const long long chunks = list.before[f + 1] - list.before[f], rel = u - a.cache.kv_heads * list.before[f];
-    const int head = (int)(rel / chunks);
-    const long long s0 = a.cache.kv_heads * list.before[f] + head * chunks;
-    if (s0 == u) return;
-    const int c0 = (int)(s0 / share), c1 = (int)((s0 + chunks - 1) / share);
+    const long long length = list.before[f + 1] - list.before[f], rel = u - a.cache.kv_heads * list.before[f];
+    const int head = (int)(rel / length);
+    const long long end = a.cache.kv_heads * list.before[f] + (head + 1) * length, s0 = end - length + kTileCost;      // its first chunk
+    if (s0 >= u) return;
+    const int c0 = (int)(s0 / share), c1 = (int)((end - 1) / share);
     if (c0 != (int)blockIdx.x) return;
     const int2 at = list.tile[f];
     const AttnRows r = attn_rows(a, at.x);

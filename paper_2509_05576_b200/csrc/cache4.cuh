@@ -303,6 +303,7 @@ struct Attn4 {
     int causal, window;
     int row_limit;                                // rows (new tokens x ratio) up to which a request is the business of the kernel for few
     int q_vec, o_vec;                             // every row of q / of out begins on 16 bytes
+    uint2 by;                                     // {64, 4} (c4_unpack4)
     float* partial;
     int32_t* status;
 };
@@ -357,10 +358,13 @@ __device__ __forceinline__ C4Factors c4_factors(uint32_t words) {
     f.off = __hneg2(__hmul2(step, zero));
     return f;
 }
-// Nibbles i of both halves of x, i = 0 .. 3.
-__device__ __forceinline__ void c4_unpack4(uint32_t x, const C4Factors& f, uint32_t (&o)[4]) {
-    const uint32_t h[4] = {((x << 6) & 0x03c003c0u) | 0x3c003c00u, ((x << 2) & 0x03c003c0u) | 0x3c003c00u,
-                           ((x >> 2) & 0x03c003c0u) | 0x3c003c00u, ((x >> 6) & 0x03c003c0u) | 0x3c003c00u};
+// Nibbles i of both halves of x, i = 0 .. 3.  The kernels that unpack are bound by the pipe of shifts and logic (two clocks an
+// instruction, 66 % busy in the one for few rows when all four shifts ran there), while that of multiplications is idle: so shifts to the left
+// are multiplications by `by` = {64, 4}, numbers that the compiler does not know and cannot make shifts of again.
+__device__ __forceinline__ void c4_unpack4(uint32_t x, const C4Factors& f, uint2 by, uint32_t (&o)[4]) {
+    const uint32_t y = x >> 8;
+    const uint32_t h[4] = {((x * by.x) & 0x03c003c0u) | 0x3c003c00u, ((x * by.y) & 0x03c003c0u) | 0x3c003c00u,
+                           ((y * by.x) & 0x03c003c0u) | 0x3c003c00u, ((y * by.y) & 0x03c003c0u) | 0x3c003c00u};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const __half2 v = __hfma2(*reinterpret_cast<const __half2*>(&h[i]), f.step16, f.off);
@@ -395,6 +399,13 @@ __device__ __forceinline__ int attn_q_shift(float top) {
     return min(14 - ((int)(__float_as_uint(top) >> 23) - 127), 126);
 }
 
+// A negative scale changes the sign of q, a scale of 0 makes it 0, and the factor that the scores still need is positive.
+__device__ __forceinline__ float attn_q_sign(float scale_log2) { return scale_log2 < 0.f ? -1.f : scale_log2 == 0.f ? 0.f : 1.f; }
+__device__ __forceinline__ float attn_score_factor(float scale_log2, int shift) {
+    // kept a finite normal number: times -infinity it has to stay -infinity, times 0 it has to stay 0
+    return scale_log2 == 0.f ? 1.f : fminf(fmaxf(fabsf(scale_log2) * exp2_int(-shift), 1.17549435e-38f), 3.4e38f);
+}
+
 // Probabilities are kept times 2^15 in fp16: down to 2^-29 of the largest they keep all their bits, and nothing above 2^-39 of it
 // is lost, so that many small ones still add up.
 constexpr float kAttnPShift = 15.f;
@@ -406,43 +417,44 @@ __device__ __forceinline__ float attn_lse(float ref, float sum, float shift) {
 template <typename T> constexpr bool kIsHalf = false;
 template <> constexpr bool kIsHalf<__half> = true;
 
-constexpr int kFewWarps = 8, kFewStages = 3, kFewThreads = 32 * kFewWarps;
-template <int HD> struct FewShape {
-    static constexpr int tiles = HD == 128 ? 2 : 4;                   // tiles of a chunk: 4608 bytes either way
-    static constexpr int chunk = tiles * kC4Tile;
-    static constexpr int chunk_bytes = tiles * c4_tile_bytes(HD);
-    static constexpr int smem_bytes = kFewWarps * kFewStages * chunk_bytes + 128;
+// One CTA an SM: twelve warps with 168 registers each, or eight with up to 255 where a lane holds the output of sixteen rows.
+__host__ __device__ constexpr int few_warps(int nt) { return nt == 1 ? 12 : 8; }
+constexpr int kFewMaxCtas = 160, kFewChunk = 64, kFewTiles = kFewChunk / kC4Tile;
+template <int HD, int NT> struct FewShape {
+    static constexpr int warps = few_warps(NT), threads = 32 * warps;
+    static constexpr int stages = HD == 128 ? 2 : 4;                  // 18432 bytes a warp either way
+    static constexpr int chunk_bytes = kFewTiles * c4_tile_bytes(HD);
+    static constexpr int smem_bytes = warps * stages * chunk_bytes + 128;
 };
 __host__ __device__ constexpr int few_partial_floats(int hd, int nt) { return 8 * nt * (hd + 2); }
-constexpr int few_max_ctas(int nt) { return nt == 1 ? 320 : 160; }
 
 // The units of all requests are dealt to the warps of the grid in equal shares, in the order (request, kv head, row tile, chunk): a
 // long request and a batch of short ones fill the GPU alike.  A warp finds its share by adding up the requests' units, 256 at a time.
-struct FewScan { long long warp[kFewWarps]; long long starts[kFewThreads]; };
-template <int kRows, int kChunk>
-__device__ __forceinline__ long long few_total(const Attn4& a, FewScan& s) {
+template <int W> struct FewScan { long long warp[W]; long long starts[32 * W]; };
+template <int kRows, int W>
+__device__ __forceinline__ long long few_total(const Attn4& a, FewScan<W>& s) {
     long long mine = 0;
-    for (int b = threadIdx.x; b < a.batch; b += kFewThreads) mine += attn_request<kRows, kChunk>(a, b).units;
+    for (int b = threadIdx.x; b < a.batch; b += 32 * W) mine += attn_request<kRows, kFewChunk>(a, b).units;
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, d);
     if ((threadIdx.x & 31) == 0) s.warp[threadIdx.x >> 5] = mine;
     __syncthreads();
     long long total = 0;
 #pragma unroll
-    for (int w = 0; w < kFewWarps; ++w) total += s.warp[w];
+    for (int w = 0; w < W; ++w) total += s.warp[w];
     __syncthreads();
     return total;
 }
 // The request that this warp's unit u belongs to and the units before it; all warps of the CTA, each with a u of its own (u >= total:
 // none).
-template <int kRows, int kChunk>
-__device__ __forceinline__ int few_find(const Attn4& a, long long u, FewScan& s, long long& before) {
+template <int kRows, int W>
+__device__ __forceinline__ int few_find(const Attn4& a, long long u, FewScan<W>& s, long long& before) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     long long base = 0;
     int found = -1;
-    for (int first = 0; first < a.batch; first += kFewThreads) {
+    for (int first = 0; first < a.batch; first += 32 * W) {
         const int b = first + threadIdx.x;
-        const long long mine = b < a.batch ? attn_request<kRows, kChunk>(a, b).units : 0;
+        const long long mine = b < a.batch ? attn_request<kRows, kFewChunk>(a, b).units : 0;
         long long x = mine;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -453,7 +465,7 @@ __device__ __forceinline__ int few_find(const Attn4& a, long long u, FewScan& s,
         __syncthreads();
         long long all = 0, at = 0;
 #pragma unroll
-        for (int w = 0; w < kFewWarps; ++w) {
+        for (int w = 0; w < W; ++w) {
             if (w == warp) at = all;
             all += s.warp[w];
         }
@@ -462,7 +474,7 @@ __device__ __forceinline__ int few_find(const Attn4& a, long long u, FewScan& s,
         if (base <= u && u < base + all) {               // the last request that starts at or before u
             int count = 0;
 #pragma unroll
-            for (int i = 0; i < kFewThreads / 32; ++i) count += __popc(__ballot_sync(0xffffffffu, s.starts[i * 32 + lane] <= u));
+            for (int i = 0; i < W; ++i) count += __popc(__ballot_sync(0xffffffffu, s.starts[i * 32 + lane] <= u));
             found = first + count - 1;
             before = s.starts[count - 1];
         }
@@ -480,13 +492,13 @@ struct FewPiece {
     int lo_any, hi_any, lo_all, hi_all;                  // keys that any, and that every row of the tile sees
     int c, c_end, last_tile;                             // its chunks that hold such keys, the end of its 16-token tiles
 };
-template <int kRows, int kChunk>
+template <int kRows>
 struct FewWalk {
     long long u, end, before;
     int b;
     __device__ __forceinline__ bool next(const Attn4& a, FewPiece& p) {
         while (u < end) {
-            p.r = attn_request<kRows, kChunk>(a, b);
+            p.r = attn_request<kRows, kFewChunk>(a, b);
             if (u >= before + p.r.units) { before += p.r.units; ++b; continue; }
             const int length = p.r.chunks + kFewTileCost, seg = (int)((u - before) / length), x0 = (int)((u - before) - (long long)seg * length);
             const int x1 = (int)min((long long)length, x0 + (end - u));
@@ -500,8 +512,8 @@ struct FewWalk {
             p.live_rows = min(kRows, p.r.rows - p.first_row);
             attn_range(a, p.r, p.first_row / a.ratio, p.lo_any, p.hi_all);
             attn_range(a, p.r, (p.first_row + p.live_rows - 1) / a.ratio, p.lo_all, p.hi_any);
-            p.c = max(p.r.chunk0 + p.from, p.lo_any / kChunk);
-            p.c_end = min(p.r.chunk0 + p.to, (p.hi_any + kChunk - 1) / kChunk);
+            p.c = max(p.r.chunk0 + p.from, p.lo_any / kFewChunk);
+            p.c_end = min(p.r.chunk0 + p.to, (p.hi_any + kFewChunk - 1) / kFewChunk);
             p.last_tile = (p.hi_any + kC4Tile - 1) / kC4Tile;
             return true;
         }
@@ -517,19 +529,19 @@ struct FewWalk {
 // Codes go from shared memory to registers as they lie and become fp16 there: three instructions for two values.
 // The order of a contraction is free, so the four lanes that share a token take 32 consecutive values each, and q is laid out alike.
 template <typename T, int HD, int NT>
-__global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) attn4_few_kernel(Attn4 a) {
-    using F = FewShape<HD>;
+__global__ void __launch_bounds__(32 * few_warps(NT), 1) attn4_few_kernel(Attn4 a) {
+    using F = FewShape<HD, NT>;
     constexpr int kRows = 8 * NT, kWords = HD / 32, kSteps = HD / 16, kTiles = HD / 16, kLane = HD / 8;
     constexpr int kSide = c4_side_bytes(HD), kTileBytes = c4_tile_bytes(HD), kCodes = kC4Tile * HD / 2, kGrids = HD / kC4Group * 2;
     extern __shared__ unsigned char few_smem_raw[];
-    __shared__ FewScan scan;
-    __shared__ uint64_t bars[kFewWarps * kFewStages];
+    __shared__ FewScan<F::warps> scan;
+    __shared__ uint64_t bars[F::warps * F::stages];
     __shared__ int abort_word;
     unsigned char* ring = few_smem_raw + (128 - (smem_u32(few_smem_raw) & 127)) % 128;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n8 = lane >> 2, t = lane & 3;
-    const unsigned char* ring_p = ring + warp * kFewStages * F::chunk_bytes;
-    const uint32_t ring_w = smem_u32(ring_p), bar_w = smem_u32(&bars[warp * kFewStages]);
-    if (lane < kFewStages) mbar_init(bar_w + 8 * lane, 1);
+    const unsigned char* ring_p = ring + warp * F::stages * F::chunk_bytes;
+    const uint32_t ring_w = smem_u32(ring_p), bar_w = smem_u32(&bars[warp * F::stages]);
+    if (lane < F::stages) mbar_init(bar_w + 8 * lane, 1);
     if (threadIdx.x == 0) abort_word = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -537,19 +549,19 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) attn4_few_kernel
     chained_begin();
 
     // workers side by side lie on different SMs: a small problem then uses as many of them as it has chunks
-    const int worker = warp * gridDim.x + blockIdx.x, workers = kFewWarps * gridDim.x;
-    const long long total = few_total<kRows, F::chunk>(a, scan), share = few_share(total, workers);
-    FewWalk<kRows, F::chunk> walk;
+    const int worker = warp * gridDim.x + blockIdx.x, workers = F::warps * gridDim.x;
+    const long long total = few_total<kRows>(a, scan), share = few_share(total, workers);
+    FewWalk<kRows> walk;
     walk.u = share * worker;
     walk.end = min(walk.u + share, total);
     walk.before = 0;
-    walk.b = few_find<kRows, F::chunk>(a, walk.u, scan, walk.before);
+    walk.b = few_find<kRows>(a, walk.u, scan, walk.before);
 
     unsigned asked = 0, done = 0;                        // chunks so far, over all pieces
     FewPiece p;
     int next = 0;
     auto ask = [&]() {                                   // the next chunk's tiles that hold keys; the whole warp
-        const int stage = asked % kFewStages, tile0 = next * F::tiles, count = min(F::tiles, p.last_tile - tile0);
+        const int stage = asked % F::stages, tile0 = next * kFewTiles, count = min(kFewTiles, p.last_tile - tile0);
         const uint32_t bar = bar_w + 8 * stage;
         if (lane == 0) mbar_arrive_expect_tx(bar, count * kTileBytes);
         __syncwarp();
@@ -565,7 +577,7 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) attn4_few_kernel
     auto begin = [&]() {
         next = p.c;
 #pragma unroll
-        for (int s = 0; s < kFewStages; ++s)
+        for (int s = 0; s < F::stages; ++s)
             if (next < p.c_end) ask();
     };
     bool more = walk.next(a, p), ok = true;
@@ -593,7 +605,7 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) attn4_few_kernel
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
             const int shift = kIsHalf<T> ? 0 : attn_q_shift(top);
-            const float f = exp2_int(shift);
+            const float f = attn_q_sign(a.scale_log2) * exp2_int(shift);
 #pragma unroll
             for (int w = 0; w < kWords; ++w)
 #pragma unroll
@@ -604,7 +616,7 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) attn4_few_kernel
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int rr = p.first_row + nt * 8 + 2 * t + h;
-                mult[nt][h] = a.scale_log2 * exp2_int(-__shfl_sync(0xffffffffu, shift, (2 * t + h) * 4));
+                mult[nt][h] = attn_score_factor(a.scale_log2, __shfl_sync(0xffffffffu, shift, (2 * t + h) * 4));
                 lo[nt][h] = hi[nt][h] = 0;
                 if (rr < p.r.rows) attn_range(a, p.r, rr / a.ratio, lo[nt][h], hi[nt][h]);
             }
@@ -623,9 +635,9 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) attn4_few_kernel
         // one chunk; `masked`: some row does not see all of it
         auto chunk = [&](const unsigned char* data, int j0, auto masked) {
             constexpr bool kMasked = decltype(masked)::value;
-            float x[NT][F::tiles][4];
+            float x[NT][kFewTiles][4];
 #pragma unroll
-            for (int tl = 0; tl < F::tiles; ++tl) {
+            for (int tl = 0; tl < kFewTiles; ++tl) {
                 const unsigned char* side = data + tl * kTileBytes;
                 alignas(16) uint32_t kw[2][kWords];
                 C4Factors f[2];
@@ -644,8 +656,8 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) attn4_few_kernel
 #pragma unroll
                 for (int w = 0; w < kWords; ++w) {
                     uint32_t k0[4], k1[4];
-                    c4_unpack4(kw[0][w], f[0], k0);
-                    c4_unpack4(kw[1][w], f[1], k1);
+                    c4_unpack4(kw[0][w], f[0], a.by, k0);
+                    c4_unpack4(kw[1][w], f[1], a.by, k1);
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -653,51 +665,52 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) attn4_few_kernel
                             mma_f16(x[nt][tl], k0[2 * h], k1[2 * h], k0[2 * h + 1], k1[2 * h + 1], qf[nt][2 * w + h][0], qf[nt][2 * w + h][1]);
                 }
             }
-            // softmax: the reference m is raised only when some score lies above it
+            // softmax: the reference m (a score, before its factor) is raised only when some score lies above it
+            float top[NT][2];
             bool above = false;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int tl = 0; tl < F::tiles; ++tl)
+                for (int h = 0; h < 2; ++h) {
+                    top[nt][h] = m[nt][h];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float v = x[nt][tl][e] * mult[nt][e & 1];
-                        if (kMasked) {
-                            const int j = j0 + tl * kC4Tile + n8 + 8 * (e >> 1);
-                            if (j < lo[nt][e & 1] || j >= hi[nt][e & 1]) v = -INFINITY;
+                    for (int tl = 0; tl < kFewTiles; ++tl)
+#pragma unroll
+                        for (int e = h; e < 4; e += 2) {
+                            if (kMasked) {
+                                const int j = j0 + tl * kC4Tile + n8 + 8 * (e >> 1);
+                                if (j < lo[nt][h] || j >= hi[nt][h]) x[nt][tl][e] = -INFINITY;
+                            }
+                            top[nt][h] = fmaxf(top[nt][h], x[nt][tl][e]);
                         }
-                        x[nt][tl][e] = v;
-                        above |= v > m[nt][e & 1];
-                    }
+                    above |= top[nt][h] > m[nt][h];
+                }
             if (__any_sync(0xffffffffu, above)) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        float top = m[nt][h];
 #pragma unroll
-                        for (int tl = 0; tl < F::tiles; ++tl) top = fmaxf(top, fmaxf(x[nt][tl][h], x[nt][tl][h + 2]));
-#pragma unroll
-                        for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-                        const float f = m[nt][h] == top ? 1.f : exp2_approx(m[nt][h] - top);      // 0 from -infinity
-                        m[nt][h] = top;
+                        for (int d = 4; d < 32; d <<= 1) top[nt][h] = fmaxf(top[nt][h], __shfl_xor_sync(0xffffffffu, top[nt][h], d));
+                        const float f = m[nt][h] == top[nt][h] ? 1.f : exp2_approx((m[nt][h] - top[nt][h]) * mult[nt][h]);    // 0 from -infinity
+                        m[nt][h] = top[nt][h];
                         l[nt][h] *= f;
 #pragma unroll
                         for (int j = 0; j < kTiles; ++j) { o[nt][j][h] *= f; o[nt][j][h + 2] *= f; }
                     }
             }
-            uint32_t pf[NT][F::tiles][2];
+            uint32_t pf[NT][kFewTiles][2];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                float ref[2];
+                float off[2];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) ref[h] = (m[nt][h] == -INFINITY ? 0.f : m[nt][h]) - kAttnPShift;
+                for (int h = 0; h < 2; ++h) off[h] = kAttnPShift - (m[nt][h] == -INFINITY ? 0.f : m[nt][h] * mult[nt][h]);
 #pragma unroll
-                for (int tl = 0; tl < F::tiles; ++tl) {
+                for (int tl = 0; tl < kFewTiles; ++tl) {
                     float pr[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        pr[e] = exp2_approx(x[nt][tl][e] - ref[e & 1]);
+                        pr[e] = exp2_approx(fmaf(x[nt][tl][e], mult[nt][e & 1], off[e & 1]));
                         l[nt][e & 1] += pr[e];
                     }
                     pf[nt][tl][0] = transpose8(pack_half2(pr[0], pr[1]));
@@ -705,7 +718,7 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) attn4_few_kernel
                 }
             }
 #pragma unroll
-            for (int tl = 0; tl < F::tiles; ++tl) {
+            for (int tl = 0; tl < kFewTiles; ++tl) {
                 const unsigned char* side = data + tl * kTileBytes + kSide;
                 constexpr int kV = HD / 64;                       // words a lane: 16 or 8 values of a token
                 alignas(8) uint32_t vw[4][kV];
@@ -727,8 +740,8 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) attn4_few_kernel
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         uint32_t v0[4], v1[4];
-                        c4_unpack4(__byte_perm(vw[0][w], vw[1][w], h ? 0x7632 : 0x5410), f0, v0);
-                        c4_unpack4(__byte_perm(vw[2][w], vw[3][w], h ? 0x7632 : 0x5410), f1, v1);
+                        c4_unpack4(__byte_perm(vw[0][w], vw[1][w], h ? 0x7632 : 0x5410), f0, a.by, v0);
+                        c4_unpack4(__byte_perm(vw[2][w], vw[3][w], h ? 0x7632 : 0x5410), f1, a.by, v1);
 #pragma unroll
                         for (int e = 0; e < 2; ++e)
 #pragma unroll
@@ -738,22 +751,26 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) attn4_few_kernel
             }
         };
         for (int c = p.c; c < p.c_end; ++c) {
-            const int stage = done % kFewStages, j0 = c * F::chunk;
-            ok = __all_sync(0xffffffffu, mbar_wait_bounded(bar_w + 8 * stage, (done / kFewStages) & 1, &abort_word));
+            const int stage = done % F::stages, j0 = c * kFewChunk;
+            ok = __all_sync(0xffffffffu, mbar_wait_bounded(bar_w + 8 * stage, (done / F::stages) & 1, &abort_word));
             if (!ok) break;
             ++done;
-            if (j0 >= p.lo_all && j0 + F::chunk <= p.hi_all) chunk(ring_p + stage * F::chunk_bytes, j0, std::false_type());
+            if (j0 >= p.lo_all && j0 + kFewChunk <= p.hi_all) chunk(ring_p + stage * F::chunk_bytes, j0, std::false_type());
             else chunk(ring_p + stage * F::chunk_bytes, j0, std::true_type());
             __syncwarp();                                         // the stage has been read
             if (next < p.c_end) ask();
         }
         if (!ok) {                                                // copies in flight land before the CTA is left
-            for (; done < asked; ++done) drain_copy(bar_w + 8 * (done % kFewStages), (done / kFewStages) & 1);
+            for (; done < asked; ++done) drain_copy(bar_w + 8 * (done % F::stages), (done / F::stages) & 1);
             if (lane == 0) report(a.status, PTQ_ERR_TIMEOUT, blockIdx.x, 3);
             break;
         }
         // the next piece's first chunks are under way while this one's results are written
         const FewPiece old = p;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) m[nt][h] = m[nt][h] == -INFINITY ? -INFINITY : m[nt][h] * mult[nt][h];
         more = walk.next(a, p);
         if (more) begin();
         const bool complete = old.from == 0 && old.to == old.r.chunks;
@@ -786,26 +803,25 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) attn4_few_kernel
 }
 
 // Joins the partial results of row tiles that several warps shared.  Warp w of CTA c looks at the border behind worker
-// c 8 + w: if it is the first one inside a tile, the CTA adds up that tile's pieces, in their order: a warp a row, or, where
+// 8 c + w: if it is the first one inside a tile, the CTA adds up that tile's pieces, in their order: a warp a row, or, where
 // the pieces are many, all warps a row together, each an eighth of the pieces.
-constexpr int kJoinTogether = 16;
+constexpr int kJoinTogether = 16, kJoinWarps = 8, kJoinThreads = 32 * kJoinWarps;
 template <typename T, int HD, int NT>
-__global__ void __launch_bounds__(kFewThreads) attn4_join_kernel(Attn4 a, int ctas) {
-    using F = FewShape<HD>;
+__global__ void __launch_bounds__(kJoinThreads) attn4_join_kernel(Attn4 a, int ctas) {
     constexpr int kRows = 8 * NT, kLane = HD / 32;
-    __shared__ FewScan scan;
+    __shared__ FewScan<kJoinWarps> scan;
     struct Job { int b, head, tile, w0, w1; };
-    __shared__ Job jobs[kFewWarps];
-    __shared__ float part_top[kFewWarps], part_sum[kFewWarps], part_v[kFewWarps][HD];
+    __shared__ Job jobs[kJoinWarps];
+    __shared__ float part_top[kJoinWarps], part_sum[kJoinWarps], part_v[kJoinWarps][HD];
     chained_begin();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, workers = ctas * kFewWarps, border = blockIdx.x * kFewWarps + warp;
-    const long long total = few_total<kRows, F::chunk>(a, scan), share = few_share(total, workers), u = share * (border + 1);
-    if (share * (blockIdx.x * kFewWarps + 1) >= total) return;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, workers = ctas * few_warps(NT), border = blockIdx.x * kJoinWarps + warp;
+    const long long total = few_total<kRows>(a, scan), share = few_share(total, workers), u = share * (border + 1);
+    if (share * (blockIdx.x * kJoinWarps + 1) >= total) return;
     long long before = 0;
-    const int b = few_find<kRows, F::chunk>(a, u, scan, before);
+    const int b = few_find<kRows>(a, u, scan, before);
     Job mine{-1, 0, 0, 0, 0};
     if (b >= 0) {
-        const AttnRequest r = attn_request<kRows, F::chunk>(a, b);
+        const AttnRequest r = attn_request<kRows, kFewChunk>(a, b);
         const int length = r.chunks + kFewTileCost, seg = (int)((u - before) / length);
         const long long s0 = before + (long long)seg * length + kFewTileCost;          // its first chunk
         const long long w0 = s0 / share, w1 = (s0 + r.chunks - 1) / share;
@@ -824,14 +840,14 @@ __global__ void __launch_bounds__(kFewThreads) attn4_join_kernel(Attn4 a, int ct
         for (int i = 0; i < kLane; ++i) out[i] = from_f32<T>(v[i] * inv);
         if (lane == 0 && a.lse) a.lse[(int64_t)(r.row0 + i0) * a.q_heads + qh] = attn_lse(ref, sum, kAttnPShift);
     };
-    for (int k = 0; k < kFewWarps; ++k) {
+    for (int k = 0; k < kJoinWarps; ++k) {
         const Job j = jobs[k];
         if (j.b < 0) continue;
-        const AttnRequest r = attn_request<kRows, F::chunk>(a, j.b);
+        const AttnRequest r = attn_request<kRows, kFewChunk>(a, j.b);
         const int live_rows = min(kRows, r.rows - j.tile * kRows);
         const bool together = j.w1 - j.w0 >= kJoinTogether;
-        for (int row = together ? 0 : warp; row < live_rows; row += together ? 1 : kFewWarps) {
-            const int step = together ? kFewWarps : 1, w_first = j.w0 + (together ? warp : 0);
+        for (int row = together ? 0 : warp; row < live_rows; row += together ? 1 : kJoinWarps) {
+            const int step = together ? kJoinWarps : 1, w_first = j.w0 + (together ? warp : 0);
             float top = -INFINITY, sum = 0.f, v[kLane];
 #pragma unroll
             for (int i = 0; i < kLane; ++i) v[i] = 0.f;
@@ -857,11 +873,11 @@ __global__ void __launch_bounds__(kFewThreads) attn4_join_kernel(Attn4 a, int ct
             __syncthreads();
             if (warp == 0) {
                 float all_top = -INFINITY, all = 0.f, w[kLane];
-                for (int q = 0; q < kFewWarps; ++q) all_top = fmaxf(all_top, part_top[q]);
+                for (int q = 0; q < kJoinWarps; ++q) all_top = fmaxf(all_top, part_top[q]);
                 const float all_ref = all_top == -INFINITY ? 0.f : all_top;
 #pragma unroll
                 for (int i = 0; i < kLane; ++i) w[i] = 0.f;
-                for (int q = 0; q < kFewWarps; ++q) {
+                for (int q = 0; q < kJoinWarps; ++q) {
                     const float f = exp2_approx(part_top[q] - all_ref);
                     all += f * part_sum[q];
 #pragma unroll

@@ -129,7 +129,7 @@ int cache_tokens(bool append, const Cache4& c, int head_dim, C4Tokens a, int typ
 
 template <typename T, int HD, int NT>
 cudaError_t allow_attn_smem() {
-    return cudaFuncSetAttribute(attn4_few_kernel<T, HD, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewShape<HD>::smem_bytes);
+    return cudaFuncSetAttribute(attn4_few_kernel<T, HD, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewShape<HD, NT>::smem_bytes);
 }
 template <typename T>
 cudaError_t allow_attn_smem_all() {
@@ -144,14 +144,15 @@ cudaError_t allow_attn_smem_all() {
 
 template <typename T, int HD, int NT>
 void attn_few_launch(const Attn4& a, int sms, cudaStream_t stream) {
-    const int want = sms * (NT == 1 ? 2 : 1), ctas = want < few_max_ctas(NT) ? want : few_max_ctas(NT);
+    using F = FewShape<HD, NT>;
+    const int ctas = sms < kFewMaxCtas ? sms : kFewMaxCtas;
     {
         Launch l(K_CACHE_ATTN_FEW, stream);
-        launch_chained(attn4_few_kernel<T, HD, NT>, ctas, kFewThreads, FewShape<HD>::smem_bytes, stream, a);
+        launch_chained(attn4_few_kernel<T, HD, NT>, ctas, F::threads, F::smem_bytes, stream, a);
     }
     {
         Launch l(K_CACHE_ATTN_JOIN, stream);
-        launch_chained(attn4_join_kernel<T, HD, NT>, ctas, kFewThreads, 0, stream, a, ctas);
+        launch_chained(attn4_join_kernel<T, HD, NT>, cdiv(ctas * F::warps, kJoinWarps), kJoinThreads, 0, stream, a, ctas);
     }
 }
 template <typename T, int HD>
@@ -185,7 +186,7 @@ AttnSpace attn_space(void* ws, int ratio, int head_dim, int batch, int total_q, 
     Carver cv(ws);
     const int64_t rows = (int64_t)max_q * ratio;
     const int nt = rows <= 8 ? 1 : 2;
-    s.few = cv.take<float>((size_t)2 * few_max_ctas(nt) * kFewWarps * few_partial_floats(head_dim, nt));
+    s.few = cv.take<float>((size_t)2 * kFewMaxCtas * few_warps(nt) * few_partial_floats(head_dim, nt));
     if (rows > kFewRows) {
         s.tiles = cv.take<float>((size_t)2 * kTileMaxCtas * tile_partial_floats(head_dim));
         s.list.most = (int)((int64_t)total_q * ratio / kTileRows) + batch;           // a last, partly filled tile for each request
@@ -355,7 +356,7 @@ int ptq_cache_attention(void* out, int64_t o_token, int64_t o_head, float* lse, 
     int st = cache_check(&a.cache, pages, num_pages, page_size, kv_heads, head_dim);
     if (st) return st;
     if (q_heads < 1 || q_heads % kv_heads || batch < 0 || total_q < 0 || max_q < 0 || max_pages < 0 || ld_table < max_pages || window < 0 ||
-        (causal != 0 && causal != 1) || (type != PTQ_F16 && type != PTQ_BF16) || !(scale - scale == 0.f))
+        (causal != 0 && causal != 1) || (type != PTQ_F16 && type != PTQ_BF16) || !(fabsf(scale) <= 2.0e38f))
         return PTQ_ERR_INVALID_ARG;
     if (batch == 0 || total_q == 0 || max_q == 0) return PTQ_OK;
     if (!out || !q || !kv_lens || !cu_q || (max_pages > 0 && !block_table) || o_token < head_dim || o_head < head_dim || q_token < 0 || q_head < 0)
@@ -387,6 +388,7 @@ int ptq_cache_attention(void* out, int64_t o_token, int64_t o_head, float* lse, 
     a.scale_log2 = scale * 1.4426950408889634f;
     a.causal = causal; a.window = window;
     a.q_vec = rows_aligned(q, q_token, q_head, 2); a.o_vec = rows_aligned(out, o_token, o_head, 2);
+    a.by = make_uint2(64u, 4u);
     a.status = status;
     const AttnSpace space = attn_space(ws, a.ratio, head_dim, batch, total_q, max_q);
     auto launch = [&](auto* t) {
