@@ -184,6 +184,19 @@ __device__ __forceinline__ uint32_t tile_at(int rows, int row, int c) {
     return (uint32_t)((c >> 3) * rows * 128 + row * 128 + (((c & 7) ^ (row & 7)) << 4));
 }
 
+// Two float32 operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)),
+        "l"(*reinterpret_cast<unsigned long long*>(&c)));
+    return *reinterpret_cast<float2*>(&r);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    unsigned long long r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)));
+    return *reinterpret_cast<float2*>(&r);
+}
+
 // Keys [lo, hi) of a row among the 32 from `at` on, a bit each.
 __device__ __forceinline__ uint32_t tile_seen(int lo, int hi, int at) {
     const int a = min(max(lo - at, 0), 32), b = min(max(hi - at, 0), 32);
@@ -211,7 +224,7 @@ __device__ __forceinline__ float tile_max(uint32_t s_tmem, int lo, int hi) {
 }
 template <bool kWhole>
 __device__ __forceinline__ float tile_probs(uint32_t s_tmem, float mult, float off, int lo, int hi) {
-    float part[4] = {0.f, 0.f, 0.f, 0.f};
+    float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
     uint32_t r[2][32];
     tc_ld32(s_tmem, r[0]);
 #pragma unroll
@@ -222,19 +235,18 @@ __device__ __forceinline__ float tile_probs(uint32_t s_tmem, float mult, float o
         if (ch < 3) tc_ld32(s_tmem + (ch + 1) * 32, r[(ch + 1) & 1]);
 #pragma unroll
         for (int e = 0; e < 32; e += 2) {
-            float v0 = exp2_approx(fmaf(__uint_as_float(r[ch & 1][e]), mult, off));
-            float v1 = exp2_approx(fmaf(__uint_as_float(r[ch & 1][e + 1]), mult, off));
+            const float2 x = fma2(make_float2(__uint_as_float(r[ch & 1][e]), __uint_as_float(r[ch & 1][e + 1])), make_float2(mult, mult), make_float2(off, off));
+            float v0 = exp2_approx(x.x), v1 = exp2_approx(x.y);
             if (!kWhole) {
                 v0 = seen >> e & 1u ? v0 : 0.f;
                 v1 = seen >> (e + 1) & 1u ? v1 : 0.f;
             }
-            part[e & 3] += v0;
-            part[(e & 3) + 1] += v1;
+            part[(e >> 1) & 1] = add2(part[(e >> 1) & 1], make_float2(v0, v1));
             w[e >> 1] = pack_half2(v0, v1);
         }
         tc_st16(s_tmem + ch * 16, w);
     }
-    return (part[0] + part[1]) + (part[2] + part[3]);
+    return (part[0].x + part[0].y) + (part[1].x + part[1].y);
 }
 
 template <typename T, int HD>
@@ -289,7 +301,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn4_tile_kernel(Attn4 a, Ti
 
     if (warp < 8) {
         // ------------------------------------------------------------ softmax: a row a thread
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
         const int t = warp >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, s_tmem = tmem + lanes + t * 128, o_tmem = tmem + lanes + 256 + t * 128;
         unsigned char* q_smem = base_ptr + t * (S::q_bytes / 2);
@@ -304,33 +316,45 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn4_tile_kernel(Attn4 a, Ti
             float mult = 0.f;
             {
                 const T* q = static_cast<const T*>(a.q) + (int64_t)(p.r.row0 + i) * a.q_token + (int64_t)qh * a.q_head;
+                uint4 raw[HD / 8];                       // the whole row at once: one trip to memory
+                if (live && a.q_vec) {
+#pragma unroll
+                    for (int c = 0; c < HD / 8; ++c) raw[c] = __ldg(reinterpret_cast<const uint4*>(q) + c);
+                } else {
+#pragma unroll
+                    for (int c = 0; c < HD / 8; ++c) {
+                        T* e = reinterpret_cast<T*>(&raw[c]);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) e[k] = live ? q[8 * c + k] : from_f32<T>(0.f);
+                    }
+                }
                 float top = 0.f;
                 bool bad = false;
-                for (int c = 0; c < HD / 8; ++c) {
-                    float v[8];
-                    load8<T>(q + 8 * c, live ? 8 : 0, a.q_vec, v);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) { top = fmaxf(top, fabsf(v[e])); bad |= not_finite(v[e]); }
-                }
+                for (int c = 0; c < HD / 8; ++c)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float v = to_f32<T>(reinterpret_cast<const T*>(&raw[c])[e]);
+                        top = fmaxf(top, fabsf(v));
+                        bad |= not_finite(v);
+                    }
                 const int shift = kIsHalf<T> || bad ? 0 : attn_q_shift(top);
                 const float f = attn_q_sign(a.scale_log2) * exp2_int(shift);
                 mult = attn_score_factor(a.scale_log2, shift);
+#pragma unroll
                 for (int c = 0; c < HD / 8; ++c) {
                     float v[8];
-                    load8<T>(q + 8 * c, live ? 8 : 0, a.q_vec, v);
-                    uint4 w;
-                    w.x = pack_half2(v[0] * f, v[4] * f);
-                    w.y = pack_half2(v[1] * f, v[5] * f);
-                    w.z = pack_half2(v[2] * f, v[6] * f);
-                    w.w = pack_half2(v[3] * f, v[7] * f);
-                    *reinterpret_cast<uint4*>(q_smem + tile_at(128, row, c)) = w;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = to_f32<T>(reinterpret_cast<const T*>(&raw[c])[e]) * f;
+                    *reinterpret_cast<uint4*>(q_smem + tile_at(128, row, c)) =
+                        make_uint4(pack_half2(v[0], v[4]), pack_half2(v[1], v[5]), pack_half2(v[2], v[6]), pack_half2(v[3], v[7]));
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 mbar_arrive(q_full(t));
             }
             int lo = 0, hi = 0;
             if (live) attn_range(a, p.r, i, lo, hi);
-            float ref = -INFINITY, sum = 0.f;
+            float ref = live ? -INFINITY : 0.f, sum = 0.f;       // rows that do not exist see nothing and need no reference
             for (int c = p.from; c < p.to; ++c) {
                 ok = __all_sync(0xffffffffu, mbar_wait_bounded(s_full(t), s_phase, abort_flag));
                 if (!ok) break;
@@ -390,7 +414,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn4_tile_kernel(Attn4 a, Ti
         if (!ok && lane == 0) *abort_flag = 1;
     } else if (warp < 12) {
         // ------------------------------------------------------------ unpacking
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 112;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         constexpr int kK = HD / 32, kV = HD / 64;              // 16-byte pieces: a key; half a value
         const int u = threadIdx.x - 256, half = (warp - 8) & 1, dims = (warp - 8) >> 1, pair = half * 64 + 2 * lane;
         struct Raw { uint4 k[kK], v[2][kV]; uint32_t kg[kK / 2], vg[2]; } now, ahead;
@@ -472,7 +496,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn4_tile_kernel(Attn4 a, Ti
             }
         }
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
         if (warp == 12) {
         // ------------------------------------------------------------ products
         int stage = 0;
