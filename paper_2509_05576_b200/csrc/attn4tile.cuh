@@ -456,7 +456,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn4_tile_kernel(Attn4 a, Ti
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     uint32_t o[4];
-                    c4_unpack4(kw[4 * g + e], f, a.by, o);
+                    c4_unpack4(kw[4 * g + e], kw[4 * g + e] >> 8, f, a.by, o);
                     *reinterpret_cast<uint4*>(stage + tile_at(kTileKeys, u, 4 * g + e)) = make_uint4(o[0], o[1], o[2], o[3]);
                 }
             }
@@ -470,7 +470,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn4_tile_kernel(Attn4 a, Ti
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         uint32_t o[4];
-                        c4_unpack4(__byte_perm(va[e], vb[e], h ? 0x7632 : 0x5410), f, a.by, o);
+                        c4_unpack4(__byte_perm(va[e], vb[e], h ? 0x7632 : 0x5410), __byte_perm(va[e], vb[e], h ? 0x0703 : 0x0501), f, a.by, o);
 #pragma unroll
                         for (int d = 0; d < 4; ++d) {
                             const int dim = dims * (HD / 2) + g * 32 + e * 8 + h * 4 + d;

@@ -361,8 +361,8 @@ __device__ __forceinline__ C4Factors c4_factors(uint32_t words) {
 // Nibbles i of both halves of x, i = 0 .. 3.  The kernels that unpack are bound by the pipe of shifts and logic (two clocks an
 // instruction, 66 % busy in the one for few rows when all four shifts ran there), while that of multiplications is idle: so shifts to the left
 // are multiplications by `by` = {64, 4}, numbers that the compiler does not know and cannot make shifts of again.
-__device__ __forceinline__ void c4_unpack4(uint32_t x, const C4Factors& f, uint2 by, uint32_t (&o)[4]) {
-    const uint32_t y = x >> 8;
+// x: nibbles 0 and 1 of its halves are taken, y: likewise, nibbles 2 and 3 that stand where 0 and 1 are in x.
+__device__ __forceinline__ void c4_unpack4(uint32_t x, uint32_t y, const C4Factors& f, uint2 by, uint32_t (&o)[4]) {
     const uint32_t h[4] = {((x * by.x) & 0x03c003c0u) | 0x3c003c00u, ((x * by.y) & 0x03c003c0u) | 0x3c003c00u,
                            ((y * by.x) & 0x03c003c0u) | 0x3c003c00u, ((y * by.y) & 0x03c003c0u) | 0x3c003c00u};
 #pragma unroll
@@ -656,8 +656,8 @@ __global__ void __launch_bounds__(32 * few_warps(NT), 1) attn4_few_kernel(Attn4 
 #pragma unroll
                 for (int w = 0; w < kWords; ++w) {
                     uint32_t k0[4], k1[4];
-                    c4_unpack4(kw[0][w], f[0], a.by, k0);
-                    c4_unpack4(kw[1][w], f[1], a.by, k1);
+                    c4_unpack4(kw[0][w], kw[0][w] >> 8, f[0], a.by, k0);
+                    c4_unpack4(kw[1][w], kw[1][w] >> 8, f[1], a.by, k1);
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -740,8 +740,8 @@ __global__ void __launch_bounds__(32 * few_warps(NT), 1) attn4_few_kernel(Attn4 
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         uint32_t v0[4], v1[4];
-                        c4_unpack4(__byte_perm(vw[0][w], vw[1][w], h ? 0x7632 : 0x5410), f0, a.by, v0);
-                        c4_unpack4(__byte_perm(vw[2][w], vw[3][w], h ? 0x7632 : 0x5410), f1, a.by, v1);
+                        c4_unpack4(__byte_perm(vw[0][w], vw[1][w], h ? 0x7632 : 0x5410), __byte_perm(vw[0][w], vw[1][w], h ? 0x0703 : 0x0501), f0, a.by, v0);
+                        c4_unpack4(__byte_perm(vw[2][w], vw[3][w], h ? 0x7632 : 0x5410), __byte_perm(vw[2][w], vw[3][w], h ? 0x0703 : 0x0501), f1, a.by, v1);
 #pragma unroll
                         for (int e = 0; e < 2; ++e)
 #pragma unroll
