@@ -377,9 +377,8 @@ f8_product_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constan
 constexpr int kF8FewThreads = 192, kF8ScaleBlocks = 16;
 template <int NT> struct F8Few {
     static constexpr int stage_bytes = (128 + NT) * kF8Block;
-    static constexpr int stages = NT <= 32 ? 5 : NT <= 64 ? 4 : 3;
-    static constexpr int bufs = NT <= 64 ? 4 : 2;
-    static constexpr int columns = bufs * NT;                                  // 64, 128 or 256: two CTAs fit an SM
+    static constexpr int stages = NT <= 32 ? 5 : 4, bufs = 4;                  // 93 to 106 KB and 64 to 256 columns: two CTAs fit an SM
+    static constexpr int columns = bufs * NT;
     static constexpr int scale_bytes = 2 * kF8ScaleBlocks * NT * 4;
     static constexpr int smem_bytes = 1024 + stages * stage_bytes + scale_bytes + 256;
     static_assert(NT * 128 * 4 <= stages * stage_bytes, "the sums go where the stages were");

@@ -52,7 +52,6 @@ cudaError_t allow_f8_smem() {
     if (e == cudaSuccess) e = allow_few_smem<T, 16>();
     if (e == cudaSuccess) e = allow_few_smem<T, 32>();
     if (e == cudaSuccess) e = allow_few_smem<T, 64>();
-    if (e == cudaSuccess) e = allow_few_smem<T, 128>();
     return e;
 }
 
@@ -68,10 +67,18 @@ int f8_few_launch(const F8Product& p, const uint8_t* A, int64_t lda, const uint8
     return PTQ_OK;
 }
 
+// Which kernel, how many rows of A a tile holds and how many CTAs share a tile's k blocks.  Measured, us (bf16 results, operands from
+// memory), rows a tile / CTAs a tile, `many` the persistent kernel:
+//   1 x 4096 x 4096: 16/1 9.3, 16/4 6.2, 16/8 6.7;  16 x 4096 x 11008: 16/1 24.1, 16/4 13.3, 16/8 12.4;  1 x 11008 x 4096: 16/1 12.3, 16/4 14.9
+//   64 x 4096 x 4096: 64/1 16.4, 64/4 11.8, 64/8 10.9;  333 x 1000 x 2048: 64/1 10.4, 64/4 11.7, 128/1 14.9, many 12.9
+//   333 x 4096 x 4096: 64/1 21.3, 64/4 37, 128/1 24.7, many 21.1;  1000 x 2048 x 2048: 64/1 13.9, many 12.9;  2048 x 4096 x 4096: 81, many 41.1
+// So: k is shared by four or eight CTAs while all of them are on the GPU at once (two an SM) and each keeps eight blocks, or four where
+// one an SM is enough (two CTAs a tile were slower than either one or four); tiles of more than 64 rows never pay; and the
+// persistent kernel takes over where its tiles fill two fifths of the SMs.
 template <typename T>
 int f8_launch(const F8Product& p, const uint8_t* A, int64_t lda, const uint8_t* B, int64_t ldb, int sms, cudaStream_t stream) {
     const long tiles_m = cdiv(p.m, kF8TileM), tiles_n = cdiv(p.n, kF8TileN);
-    if (tiles_m * tiles_n >= sms) {
+    if (5 * tiles_m * tiles_n >= 2 * sms) {
         CUtensorMap mapA, mapB;
         int st = f8_map(&mapA, A, p.m, p.k, lda, kF8TileM);
         if (!st) st = f8_map(&mapB, B, p.n, p.k, ldb, kF8TileN);
@@ -81,16 +88,16 @@ int f8_launch(const F8Product& p, const uint8_t* A, int64_t lda, const uint8_t* 
         launch_chained(f8_product_kernel<T>, grid, kF8Threads, kF8SmemBytes, stream, mapA, mapB, p, (int)tiles_m, (int)tiles_n);
         return PTQ_OK;
     }
-    const int nt = p.m <= 16 ? 16 : p.m <= 32 ? 32 : p.m <= 64 ? 64 : 128;
+    const int nt = p.m <= 16 ? 16 : p.m <= 32 ? 32 : 64;
     const long tiles = (long)cdiv(p.n, 128) * cdiv(p.m, nt);
     int ks = 1;
-    while (ks < 8 && tiles * ks * 2 <= 2 * sms && ks * 2 <= p.kb) ks *= 2;
+    for (int c = 4; c <= 8; c *= 2)
+        if ((tiles * c <= 2 * sms && p.kb >= 8 * c) || (tiles * c <= sms && p.kb >= 4 * c)) ks = c;
     switch (nt) {
         case 16: return f8_few_launch<T, 16>(p, A, lda, B, ldb, ks, stream);
         case 32: return f8_few_launch<T, 32>(p, A, lda, B, ldb, ks, stream);
-        case 64: return f8_few_launch<T, 64>(p, A, lda, B, ldb, ks, stream);
     }
-    return f8_few_launch<T, 128>(p, A, lda, B, ldb, ks, stream);
+    return f8_few_launch<T, 64>(p, A, lda, B, ldb, ks, stream);
 }
 
 int cache_check(Cache4* c, const void* pages, int num_pages, int page_size, int kv_heads, int head_dim) {
