@@ -184,19 +184,6 @@ __device__ __forceinline__ uint32_t tile_at(int rows, int row, int c) {
     return (uint32_t)((c >> 3) * rows * 128 + row * 128 + (((c & 7) ^ (row & 7)) << 4));
 }
 
-// Two float32 operations in one instruction.
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-    unsigned long long r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)),
-        "l"(*reinterpret_cast<unsigned long long*>(&c)));
-    return *reinterpret_cast<float2*>(&r);
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-    unsigned long long r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)));
-    return *reinterpret_cast<float2*>(&r);
-}
-
 // Keys [lo, hi) of a row among the 32 from `at` on, a bit each.
 __device__ __forceinline__ uint32_t tile_seen(int lo, int hi, int at) {
     const int a = min(max(lo - at, 0), 32), b = min(max(hi - at, 0), 32);

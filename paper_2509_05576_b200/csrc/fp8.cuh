@@ -44,6 +44,19 @@ __device__ __forceinline__ void load8(const T* __restrict__ p, int n, bool vec, 
     }
 }
 
+// Two float32 operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)),
+        "l"(*reinterpret_cast<unsigned long long*>(&c)));
+    return *reinterpret_cast<float2*>(&r);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    unsigned long long r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)));
+    return *reinterpret_cast<float2*>(&r);
+}
+
 __device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
 
 // Exponent e of the scale of a block whose largest magnitude is `top`: 448 = 1.75 2^8, so the mantissa of top decides by 1.75.
@@ -75,29 +88,22 @@ __device__ __forceinline__ void f8_store8(uint8_t* p, int n, uint2 c) {
 constexpr uint32_t kF8NanCodes = 0x7f7f7f7fu;
 
 // One scale per row and block of 128 columns: sixteen lanes hold a block, eight values each.  Bound by memory (one read of x,
-// one write of the codes); kF8RowUnroll blocks a thread keep that many 16-byte loads in flight.
+// one write of the codes); a thread has kF8RowUnroll blocks of its row, that many 16-byte loads in flight.
 constexpr int kF8RowUnroll = 4;
 template <typename T>
 __global__ void __launch_bounds__(256) f8_quantize_rows_kernel(const T* __restrict__ x, int rows, int cols, int64_t ldx, int vec,
                                                                 uint8_t* __restrict__ q, int64_t ldq, float* __restrict__ scale,
                                                                 int64_t lds, int32_t* status) {
     chained_begin();
-    const int kb = (cols + kF8Block - 1) / kF8Block, sub = threadIdx.x & 15;
-    const int64_t total = (int64_t)rows * kb;
-    const int64_t u0 = (int64_t)blockIdx.x * (16 * kF8RowUnroll) + (threadIdx.x >> 4);
+    const int kb = (cols + kF8Block - 1) / kF8Block, sub = threadIdx.x & 15, first = blockIdx.y * kF8RowUnroll;
+    const int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+    if (row >= rows) return;                              // the half warps of a row stay or leave together
+    const unsigned half = 0xffffu << (threadIdx.x & 16);
     float v[kF8RowUnroll][8];
-    int row[kF8RowUnroll], blk[kF8RowUnroll];
 #pragma unroll
     for (int i = 0; i < kF8RowUnroll; ++i) {
-        const int64_t u = u0 + i * 16;
-        row[i] = -1;
-        blk[i] = 0;
-        if (u < total) {
-            row[i] = (int)(u / kb);
-            blk[i] = (int)(u - (int64_t)row[i] * kb);
-        }
-        const int c0 = blk[i] * kF8Block + sub * 8;
-        load8<T>(x + (int64_t)(row[i] < 0 ? 0 : row[i]) * ldx + c0, row[i] < 0 ? 0 : cols - c0, vec, v[i]);
+        const int c0 = (first + i) * kF8Block + sub * 8;
+        load8<T>(x + row * ldx + c0, cols - c0, vec, v[i]);
     }
 #pragma unroll
     for (int i = 0; i < kF8RowUnroll; ++i) {
@@ -107,16 +113,17 @@ __global__ void __launch_bounds__(256) f8_quantize_rows_kernel(const T* __restri
         for (int j = 0; j < 8; ++j) { top = fmaxf(top, fabsf(v[i][j])); bad |= not_finite(v[i][j]); }
         if (bad) top = __uint_as_float(0x7f800000u);
 #pragma unroll
-        for (int s = 8; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
-        if (row[i] < 0) continue;
+        for (int s = 8; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor_sync(half, top, s));
+        const int blk = first + i;
+        if (blk >= kb) break;
         bad = not_finite(top);
-        const int e = f8_exponent(top), c0 = blk[i] * kF8Block + sub * 8;
+        const int e = f8_exponent(top), c0 = blk * kF8Block + sub * 8;
         uint2 codes = f8_codes8(v[i], bad ? 0.f : exp2_int(-e));
         if (bad) codes = make_uint2(kF8NanCodes, kF8NanCodes);
-        f8_store8(q + (int64_t)row[i] * ldq + c0, cols - c0, codes);
+        f8_store8(q + row * ldq + c0, cols - c0, codes);
         if (sub == 0) {
-            scale[(int64_t)row[i] * lds + blk[i]] = bad ? __uint_as_float(0x7fc00000u) : exp2_int(e);
-            if (bad) report(status, PTQ_ERR_NONFINITE, row[i]);
+            scale[row * lds + blk] = bad ? __uint_as_float(0x7fc00000u) : exp2_int(e);
+            if (bad) report(status, PTQ_ERR_NONFINITE, (int)row);
         }
     }
 }
@@ -321,6 +328,7 @@ f8_product_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constan
         uint32_t acc_phase = 0;
         bool ok = true;
         const bool vec = (p.ldc * sizeof(T)) % 16 == 0 && (reinterpret_cast<uintptr_t>(p.C) & 15) == 0;
+        const bool sa_vec = p.ldsa % 4 == 0 && (reinterpret_cast<uintptr_t>(p.sa) & 15) == 0;
         for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
             int tm, tn;
             f8_tile(tile, tiles_m, tiles_n, tm, tn);
@@ -331,30 +339,53 @@ f8_product_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constan
             float acc[kF8Block];
 #pragma unroll
             for (int c = 0; c < kF8Block; ++c) acc[c] = 0.f;
-            float next = __ldg(sa) * __ldg(sb);
-            for (int b = 0; b < p.kb; ++b) {
-                const float s = next;
-                if (b + 1 < p.kb) next = __ldg(sa + b + 1) * __ldg(sb + b + 1);
-                ok = __all_sync(0xffffffffu, mbar_wait_bounded(acc_full(buf), acc_phase, abort_flag));
-                if (!ok) break;
-                tc_fence_after();
-                const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + buf * kF8TileN + half * kF8Block;
-                // 32 columns are read while the 32 before them are added
-                uint32_t r[2][32];
-                tc_ld32(taddr, r[0]);
+            // A row's scales come four k blocks at a time and a group ahead: one by one, every lane's load was a sector of its own
+            // for each block (432 us where this takes YYY).
+            float now[4], ahead[4];
+            auto scales = [&](int b) {
+                if (sa_vec && b + 4 <= p.kb) {
+                    const float4 f = __ldg(reinterpret_cast<const float4*>(sa + b));
+                    ahead[0] = f.x; ahead[1] = f.y; ahead[2] = f.z; ahead[3] = f.w;
+                } else {
 #pragma unroll
-                for (int ch = 0; ch < kF8Block / 32; ++ch) {
-                    tc_wait_ld();
-                    if (ch + 1 < kF8Block / 32) {
-                        tc_ld32(taddr + (ch + 1) * 32, r[(ch + 1) & 1]);
-                    } else {
-                        tc_fence_before();
-                        mbar_arrive(acc_empty(buf));
-                    }
-#pragma unroll
-                    for (int c = 0; c < 32; ++c) acc[ch * 32 + c] = fmaf(s, __uint_as_float(r[ch & 1][c]), acc[ch * 32 + c]);
+                    for (int j = 0; j < 4; ++j) ahead[j] = b + j < p.kb ? __ldg(sa + b + j) : 0.f;
                 }
-                if (++buf == 2) { buf = 0; acc_phase ^= 1u; }
+            };
+            scales(0);
+#pragma unroll 1
+            for (int b0 = 0; b0 < p.kb && ok; b0 += 4) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) now[j] = ahead[j] * (b0 + j < p.kb ? __ldg(sb + b0 + j) : 0.f);
+                if (b0 + 4 < p.kb) scales(b0 + 4);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (b0 + j >= p.kb || !ok) break;
+                    ok = __all_sync(0xffffffffu, mbar_wait_bounded(acc_full(buf), acc_phase, abort_flag));
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + buf * kF8TileN + half * kF8Block;
+                    // 16 columns are read while the 16 before them are added
+                    uint32_t r[2][16];
+                    tc_ld16(taddr, r[0]);
+#pragma unroll
+                    for (int ch = 0; ch < kF8Block / 16; ++ch) {
+                        tc_wait_ld();
+                        if (ch + 1 < kF8Block / 16) {
+                            tc_ld16(taddr + (ch + 1) * 16, r[(ch + 1) & 1]);
+                        } else {
+                            tc_fence_before();
+                            mbar_arrive(acc_empty(buf));
+                        }
+#pragma unroll
+                        for (int c = 0; c < 16; c += 2) {
+                            const float2 sum = fma2(make_float2(__uint_as_float(r[ch & 1][c]), __uint_as_float(r[ch & 1][c + 1])),
+                                                    make_float2(now[j], now[j]), make_float2(acc[ch * 16 + c], acc[ch * 16 + c + 1]));
+                            acc[ch * 16 + c] = sum.x;
+                            acc[ch * 16 + c + 1] = sum.y;
+                        }
+                    }
+                    if (++buf == 2) { buf = 0; acc_phase ^= 1u; }
+                }
             }
             if (ok && live) {
                 T* out = static_cast<T*>(p.C) + (int64_t)row * p.ldc + col;
