@@ -59,6 +59,13 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
 
 __device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
 
+// The larger magnitude; a NaN stays one (and an infinity is larger than anything else), so one look at the result tells.
+__device__ __forceinline__ float max_magnitude(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(fabsf(a)), "f"(fabsf(b)));
+    return r;
+}
+
 // Exponent e of the scale of a block whose largest magnitude is `top`: 448 = 1.75 2^8, so the mantissa of top decides by 1.75.
 __device__ __forceinline__ int f8_exponent(float top) {
     const int e = (int)((__float_as_uint(top) + 0x1fffffu) >> 23) - 127 - 8;
@@ -87,44 +94,33 @@ __device__ __forceinline__ void f8_store8(uint8_t* p, int n, uint2 c) {
 }
 constexpr uint32_t kF8NanCodes = 0x7f7f7f7fu;
 
-// One scale per row and block of 128 columns: sixteen lanes hold a block, eight values each.  Bound by memory (one read of x,
-// one write of the codes); a thread has kF8RowUnroll blocks of its row, that many 16-byte loads in flight.
-constexpr int kF8RowUnroll = 4;
+// One scale per row and block of 128 columns: sixteen lanes hold a block, eight values each.  One read of x, one write of the codes;
+// 16-bit inputs are bound by the instructions between them (8192 x 4096: float32 29 us, bf16 XX).  A block a half warp: two or four
+// in a row were slower (26.8, 30.8, 33.4 us with one, two, four).
 template <typename T>
 __global__ void __launch_bounds__(256) f8_quantize_rows_kernel(const T* __restrict__ x, int rows, int cols, int64_t ldx, int vec,
                                                                 uint8_t* __restrict__ q, int64_t ldq, float* __restrict__ scale,
                                                                 int64_t lds, int32_t* status) {
     chained_begin();
-    const int kb = (cols + kF8Block - 1) / kF8Block, sub = threadIdx.x & 15, first = blockIdx.y * kF8RowUnroll;
-    const int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
-    if (row >= rows) return;                              // the half warps of a row stay or leave together
+    // two blocks of eight rows: a warp's two half warps take neighbouring blocks
+    const int blk = 2 * blockIdx.y + ((threadIdx.x >> 4) & 1), c0 = blk * kF8Block + (threadIdx.x & 15) * 8;
+    const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (row >= rows || blk * kF8Block >= cols) return;    // the lanes of a half warp stay or leave together
     const unsigned half = 0xffffu << (threadIdx.x & 16);
-    float v[kF8RowUnroll][8];
+    float v[8], top = 0.f;
+    load8<T>(x + row * ldx + c0, cols - c0, vec, v);
 #pragma unroll
-    for (int i = 0; i < kF8RowUnroll; ++i) {
-        const int c0 = (first + i) * kF8Block + sub * 8;
-        load8<T>(x + row * ldx + c0, cols - c0, vec, v[i]);
-    }
+    for (int j = 0; j < 8; ++j) top = max_magnitude(top, v[j]);
 #pragma unroll
-    for (int i = 0; i < kF8RowUnroll; ++i) {
-        float top = 0.f;
-        bool bad = false;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) { top = fmaxf(top, fabsf(v[i][j])); bad |= not_finite(v[i][j]); }
-        if (bad) top = __uint_as_float(0x7f800000u);
-#pragma unroll
-        for (int s = 8; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor_sync(half, top, s));
-        const int blk = first + i;
-        if (blk >= kb) break;
-        bad = not_finite(top);
-        const int e = f8_exponent(top), c0 = blk * kF8Block + sub * 8;
-        uint2 codes = f8_codes8(v[i], bad ? 0.f : exp2_int(-e));
-        if (bad) codes = make_uint2(kF8NanCodes, kF8NanCodes);
-        f8_store8(q + row * ldq + c0, cols - c0, codes);
-        if (sub == 0) {
-            scale[row * lds + blk] = bad ? __uint_as_float(0x7fc00000u) : exp2_int(e);
-            if (bad) report(status, PTQ_ERR_NONFINITE, (int)row);
-        }
+    for (int s = 8; s > 0; s >>= 1) top = max_magnitude(top, __shfl_xor_sync(half, top, s));
+    const bool bad = not_finite(top);
+    const int e = f8_exponent(top);
+    uint2 codes = f8_codes8(v, bad ? 0.f : exp2_int(-e));
+    if (bad) codes = make_uint2(kF8NanCodes, kF8NanCodes);
+    f8_store8(q + row * ldq + c0, cols - c0, codes);
+    if ((threadIdx.x & 15) == 0) {
+        scale[row * lds + blk] = bad ? __uint_as_float(0x7fc00000u) : exp2_int(e);
+        if (bad) report(status, PTQ_ERR_NONFINITE, (int)row);
     }
 }
 
@@ -137,7 +133,6 @@ __global__ void __launch_bounds__(256) f8_quantize_blocks_kernel(const T* __rest
     __shared__ float warp_top[8];
     const int c0 = blockIdx.x * kF8Block + (threadIdx.x & 15) * 8, r0 = blockIdx.y * kF8Block + (threadIdx.x >> 4);
     float v[8][8], top = 0.f;
-    bool bad = false;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int r = r0 + 16 * i;
@@ -146,15 +141,14 @@ __global__ void __launch_bounds__(256) f8_quantize_blocks_kernel(const T* __rest
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) { top = fmaxf(top, fabsf(v[i][j])); bad |= not_finite(v[i][j]); }
-    if (bad) top = __uint_as_float(0x7f800000u);
+        for (int j = 0; j < 8; ++j) top = max_magnitude(top, v[i][j]);
 #pragma unroll
-    for (int s = 16; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+    for (int s = 16; s > 0; s >>= 1) top = max_magnitude(top, __shfl_xor_sync(0xffffffffu, top, s));
     if ((threadIdx.x & 31) == 0) warp_top[threadIdx.x >> 5] = top;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < 8; ++w) top = fmaxf(top, warp_top[w]);
-    bad = not_finite(top);
+    for (int w = 0; w < 8; ++w) top = max_magnitude(top, warp_top[w]);
+    const bool bad = not_finite(top);
     const int e = f8_exponent(top);
     const float inv = bad ? 0.f : exp2_int(-e);
 #pragma unroll

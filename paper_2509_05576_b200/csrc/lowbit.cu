@@ -233,7 +233,7 @@ int ptq_fp8_quantize(const void* x, int x_type, int rows, int cols, int64_t ldx,
     if (rows < 0 || cols < 1 || !size || (block_rows != 1 && block_rows != kF8Block)) return PTQ_ERR_INVALID_ARG;
     if (rows == 0) return PTQ_OK;
     if (!x || !q || !scale || ldx < cols || ldq < cols || ld_scale < kb) return PTQ_ERR_INVALID_ARG;
-    if (rows > 0x7fffff00 || cols > 0x7fffff00 || (block_rows > 1 ? cdiv(rows, kF8Block) : cdiv(kb, kF8RowUnroll)) > 65535) return PTQ_ERR_UNSUPPORTED;
+    if (rows > 0x7fffff00 || cols > 0x7fffff00 || (block_rows > 1 ? cdiv(rows, kF8Block) : cdiv(kb, 2)) > 65535) return PTQ_ERR_UNSUPPORTED;
     if (!aligned16(q) || ldq % 16) return PTQ_ERR_ALIGNMENT;
     const Span in = rows_span(x, rows, ldx, cols, size), codes = rows_span(q, rows, ldq, cols, 1),
                factors = rows_span(scale, cdiv(rows, block_rows), ld_scale, kb, 4);
@@ -244,7 +244,7 @@ int ptq_fp8_quantize(const void* x, int x_type, int rows, int cols, int64_t ldx,
         const T* xs = static_cast<const T*>(x);
         if (block_rows == 1) {
             Launch l(K_F8_QUANTIZE, stream);
-            launch_chained(f8_quantize_rows_kernel<T>, dim3((rows - 1) / 16 + 1, cdiv(kb, kF8RowUnroll)), 256, 0, stream, xs, rows, cols, ldx, vec, q, ldq, scale, ld_scale,
+            launch_chained(f8_quantize_rows_kernel<T>, dim3((rows - 1) / 8 + 1, cdiv(kb, 2)), 256, 0, stream, xs, rows, cols, ldx, vec, q, ldq, scale, ld_scale,
                            status);
         } else {
             Launch l(K_F8_QUANTIZE, stream);
