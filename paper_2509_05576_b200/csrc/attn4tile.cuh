@@ -7,9 +7,16 @@
 // work on the other tile.  TMEM (all 512 columns): S0, S1 (128 each), O0, O1.  P is fp16 and lies where its S was, as the operand
 // of the second product.
 //
-// Per chunk the tensor cores need 2 x 1024 clocks (heads of 128), the exponentials 2 x 1024 (16 a clock), unpacking some 550 issue slots
-// of each scheduler.  The reference of a row's exponentials is only moved when a score lies more than 2^7 above it (P then still
-// fits fp16), so that O is hardly ever rescaled.
+// Per chunk the tensor cores need 2 x 1024 clocks (heads of 128), the exponentials 2 x 1024 (16 a clock); a chunk takes some 4700.
+// 1024 and 633 tokens behind 7168 and 4430, 32 heads on 8: 195 us, 0.9 PFLOP/s.  No part bounds it alone: without the
+// exponentials, without unpacking or with an eighth of the products it is 13, 10 or 15 us faster, without all of them 76; what is left is
+// the chain scores - softmax - products of each tile, and four unpacking warps whose loads and shared-memory stores take 4300 clocks a
+// chunk.  Tried, and slower or no faster: seven unpacking warps with items unrolled (358 us: the four roles then wait for
+// instructions) or rolled (253), codes through shared memory by bulk copies (213), keys and values in stages of their own (203),
+// scores in halves of 64 keys so that a tile's next scores are formed during its softmax (238), one pass over the scores with the
+// probabilities held in registers (267).
+// The reference of a row's exponentials is only moved when a score lies more than 2^7 above it (P then still fits fp16), so that O is
+// hardly ever rescaled.
 //
 // The units (128 keys of one tile) are dealt to the CTAs in equal shares, as those of the kernel for few rows; what a row tile sees of
 // the keys differs from tile to tile, so a first small kernel lists the tiles with the units before each.
@@ -550,7 +557,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn4_tile_kernel(Attn4 a, Ti
     if (threadIdx.x == 0 && abort_word) report(a.status, PTQ_ERR_TIMEOUT, blockIdx.x, 4);
 }
 
-// Joins what CTAs share of a tile, as attn4_join_kernel does; gridDim.y slices of rows.
+// Joins what CTAs share of a tile, as attn4_join_kernel does; a CTA takes one slice of the rows.
+constexpr int kTileJoinSlices = 8;
 template <typename T, int HD>
 __global__ void __launch_bounds__(256) attn4_tile_join_kernel(Attn4 a, TileList list, int ctas) {
     constexpr int kLane = HD / 32;
@@ -569,26 +577,47 @@ __global__ void __launch_bounds__(256) attn4_tile_join_kernel(Attn4 a, TileList 
     if (c0 != (int)blockIdx.x) return;
     const int2 at = list.tile[f];
     const AttnRows r = attn_rows(a, at.x);
-    const int first = at.y * kTileRows, live = min(kTileRows, r.n * a.ratio - first), slice = kTileRows / gridDim.y;
-    for (int row = blockIdx.y * slice + warp; row < min(live, (int)(blockIdx.y + 1) * slice); row += 8) {
-        float top = -INFINITY, sum = 0.f, v[kLane];
+    // four rows a warp side by side: their loads are in flight together
+    constexpr int kJoin = kTileRows / kTileJoinSlices / 8;
+    const int first = at.y * kTileRows, live = min(kTileRows, r.n * a.ratio - first), row0 = blockIdx.y * (kTileRows / kTileJoinSlices) + warp;
+    float ref[kJoin], sum[kJoin], v[kJoin][kLane];
 #pragma unroll
-        for (int i = 0; i < kLane; ++i) v[i] = 0.f;
-        for (int c = c0; c <= c1; ++c) top = fmaxf(top, a.partial[(2 * c + (c == c0)) * tile_partial_floats(HD) + kTileRows * HD + row]);
-        const float ref = top == -INFINITY ? 0.f : top;
-        for (int c = c0; c <= c1; ++c) {
-            const float* slot = a.partial + (2 * c + (c == c0)) * tile_partial_floats(HD);
-            const float w = exp2_approx(slot[kTileRows * HD + row] - ref);
-            sum += w * slot[kTileRows * (HD + 1) + row];
+    for (int k = 0; k < kJoin; ++k) {
+        ref[k] = -INFINITY;
+        sum[k] = 0.f;
 #pragma unroll
-            for (int i = 0; i < kLane; ++i) v[i] += w * slot[row * HD + lane * kLane + i];
+        for (int i = 0; i < kLane; ++i) v[k][i] = 0.f;
+    }
+    for (int c = c0; c <= c1; ++c) {
+        const float* slot = a.partial + (2 * c + (c == c0)) * tile_partial_floats(HD);
+#pragma unroll
+        for (int k = 0; k < kJoin; ++k)
+            if (row0 + 8 * k < live) ref[k] = fmaxf(ref[k], slot[kTileRows * HD + row0 + 8 * k]);
+    }
+#pragma unroll
+    for (int k = 0; k < kJoin; ++k) ref[k] = ref[k] == -INFINITY ? 0.f : ref[k];
+    for (int c = c0; c <= c1; ++c) {
+        const float* slot = a.partial + (2 * c + (c == c0)) * tile_partial_floats(HD);
+#pragma unroll
+        for (int k = 0; k < kJoin; ++k) {
+            const int row = row0 + 8 * k;
+            if (row >= live) continue;
+            const float w = exp2_approx(slot[kTileRows * HD + row] - ref[k]);
+            sum[k] += w * slot[kTileRows * (HD + 1) + row];
+#pragma unroll
+            for (int i = 0; i < kLane; ++i) v[k][i] += w * slot[row * HD + lane * kLane + i];
         }
+    }
+#pragma unroll
+    for (int k = 0; k < kJoin; ++k) {
+        const int row = row0 + 8 * k;
+        if (row >= live) continue;
         const int rr = first + row, i0 = rr / a.ratio, qh = head * a.ratio + rr - i0 * a.ratio;
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        const float inv = sum[k] == 0.f ? 0.f : 1.f / sum[k];
         T* out = static_cast<T*>(a.out) + (int64_t)(r.row0 + i0) * a.o_token + (int64_t)qh * a.o_head + lane * kLane;
 #pragma unroll
-        for (int i = 0; i < kLane; ++i) out[i] = from_f32<T>(v[i] * inv);
-        if (lane == 0 && a.lse) a.lse[(int64_t)(r.row0 + i0) * a.q_heads + qh] = attn_lse(ref, sum, kTilePShift);
+        for (int i = 0; i < kLane; ++i) out[i] = from_f32<T>(v[k][i] * inv);
+        if (lane == 0 && a.lse) a.lse[(int64_t)(r.row0 + i0) * a.q_heads + qh] = attn_lse(ref[k], sum[k], kTilePShift);
     }
 }
 

@@ -358,10 +358,10 @@ __device__ __forceinline__ C4Factors c4_factors(uint32_t words) {
     f.off = __hneg2(__hmul2(step, zero));
     return f;
 }
-// Nibbles i of both halves of x, i = 0 .. 3.  The kernels that unpack are bound by the pipe of shifts and logic (two clocks an
-// instruction, 66 % busy in the one for few rows when all four shifts ran there), while that of multiplications is idle: so shifts to the left
-// are multiplications by `by` = {64, 4}, numbers that the compiler does not know and cannot make shifts of again.
-// x: nibbles 0 and 1 of its halves are taken, y: likewise, nibbles 2 and 3 that stand where 0 and 1 are in x.
+// Four values of either half.  The pipe of shifts and logic is the busiest one where codes are unpacked (66 % in the kernel for few rows,
+// 60 % so; the times are the same within the noise), so shifts to the left are multiplications by `by` = {64, 4}, numbers that the
+// compiler does not know and cannot make shifts of again.
+// x: the lowest two nibbles of its halves are taken; y: those two that follow, at the same place.
 __device__ __forceinline__ void c4_unpack4(uint32_t x, uint32_t y, const C4Factors& f, uint2 by, uint32_t (&o)[4]) {
     const uint32_t h[4] = {((x * by.x) & 0x03c003c0u) | 0x3c003c00u, ((x * by.y) & 0x03c003c0u) | 0x3c003c00u,
                            ((y * by.x) & 0x03c003c0u) | 0x3c003c00u, ((y * by.y) & 0x03c003c0u) | 0x3c003c00u};
@@ -522,12 +522,15 @@ struct FewWalk {
 };
 
 // Few rows (the new tokens of a request times the query heads of a kv head, up to 8 NT at a time): what counts is one read of the cache.
-// Every warp works by itself, with three chunks in flight (bulk copies of 2304 bytes, sixteen warps an SM); a row tile that lies in
-// one warp's share is finished by it, others are joined afterwards.
+// Every warp works by itself, with two chunks of 64 tokens in flight (heads of 128; bulk copies, one for a tile); a row tile that
+// lies in one warp's share is finished by it, others are joined afterwards.
 // The cache is the 16-row operand of the tensor cores and the query rows their eight columns, so that a group of up to eight query
 // heads costs half of what it would the other way round:  S^T = K q (16 tokens x 8 rows), O^T = V^T P^T (16 values x 8 rows).
 // Codes go from shared memory to registers as they lie and become fp16 there: three instructions for two values.
 // The order of a contraction is free, so the four lanes that share a token take 32 consecutive values each, and q is laid out alike.
+// Two requests of 131072 and 81007 tokens, eight heads of 128: 66 us for 244 MB (3.7 TB/s); bound by the instructions that unpack: some
+// 1600 for 64 tokens of a head, issued at 0.63 a clock, shifts and logic 60 % busy, the tensor cores 20 %.  (Sixteen warps with 32 tokens
+// a turn 79 us; a CTA on one piece, its warps joined in shared memory, 81 us, and 140 against 95 for a ragged batch of 64.)
 template <typename T, int HD, int NT>
 __global__ void __launch_bounds__(32 * few_warps(NT), 1) attn4_few_kernel(Attn4 a) {
     using F = FewShape<HD, NT>;

@@ -74,11 +74,11 @@ int f8_few_launch(const F8Product& p, const uint8_t* A, int64_t lda, const uint8
 //   333 x 4096 x 4096: 64/1 21.3, 64/4 37, 128/1 24.7, many 21.1;  1000 x 2048 x 2048: 64/1 13.9, many 12.9;  2048 x 4096 x 4096: 81, many 41.1
 // So: k is shared by four or eight CTAs while all of them are on the GPU at once (two an SM) and each keeps eight blocks, or four where
 // one an SM is enough (two CTAs a tile were slower than either one or four); tiles of more than 64 rows never pay; and the
-// persistent kernel takes over where its tiles fill two fifths of the SMs.
+// persistent kernel takes over above them where its tiles fill two fifths of the SMs.
 template <typename T>
 int f8_launch(const F8Product& p, const uint8_t* A, int64_t lda, const uint8_t* B, int64_t ldb, int sms, cudaStream_t stream) {
     const long tiles_m = cdiv(p.m, kF8TileM), tiles_n = cdiv(p.n, kF8TileN);
-    if (5 * tiles_m * tiles_n >= 2 * sms) {
+    if (p.m > 64 && 5 * tiles_m * tiles_n >= 2 * sms) {
         CUtensorMap mapA, mapB;
         int st = f8_map(&mapA, A, p.m, p.k, lda, kF8TileM);
         if (!st) st = f8_map(&mapB, B, p.n, p.k, ldb, kF8TileN);
@@ -175,7 +175,7 @@ void attn_tile_launch(const Attn4& a, const TileList& list, int sms, cudaStream_
     }
     {
         Launch l(K_CACHE_ATTN_TILE_JOIN, stream);
-        launch_chained(attn4_tile_join_kernel<T, HD>, dim3(ctas - 1, 8), 256, 0, stream, a, list, ctas);
+        launch_chained(attn4_tile_join_kernel<T, HD>, dim3(ctas - 1, kTileJoinSlices), 256, 0, stream, a, list, ctas);
     }
 }
 

@@ -7,6 +7,7 @@ or no CUDA device is present, the calls raise.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from ctypes import c_double, c_float, c_int, c_int64, c_size_t, c_void_p
 
@@ -438,7 +439,7 @@ def _status_ptr(status, dev):
 def _call(fn, dev, stream, *args):
     """fn(*args, stream) with device `dev` current, on its current stream unless one is given."""
     raw = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
-    if torch.cuda.current_device() == dev:
+    if torch._C._cuda_getDevice() == dev:
         ret = fn(*args, raw)
     else:
         with torch.cuda.device(dev):
@@ -538,6 +539,11 @@ def cache_read(cache, slots, k, v, status, stream=None):
     _cache_tokens(lib().ptq_cache_read, cache, k, v, slots, status, stream)
 
 
+@functools.lru_cache(maxsize=1024)
+def _attention_workspace_bytes(*sizes):
+    return int(lib().ptq_cache_attention_workspace_bytes(*sizes))
+
+
 def cache_attention(out, q, cache, block_table, kv_lens, cu_q, max_q, scale, ws, status, causal=True, window=0, lse=None,
                     stream=None):
     """Attention of the newest tokens of each request (rows cu_q[r] .. cu_q[r + 1] - 1 of q [tokens, q_heads, head_dim]) over the
@@ -553,7 +559,7 @@ def cache_attention(out, q, cache, block_table, kv_lens, cu_q, max_q, scale, ws,
     if lse is not None:
         plse, ld = _matrix(lse, tokens, q_heads, _F32, dev, "lse")
         _expect(ld == q_heads, "lse must be contiguous")
-    need = lib().ptq_cache_attention_workspace_bytes(q_heads, cache.kv_heads, cache.head_dim, batch, tokens, max_q)
+    need = _attention_workspace_bytes(q_heads, cache.kv_heads, cache.head_dim, batch, tokens, max_q)
     buf = ws.get(need)
     _expect(buf.get_device() == dev, f"the workspace is on {buf.device}, the tensors are on cuda:{dev}")
     _call(lib().ptq_cache_attention, dev, stream, *_heads(out, *shape, "out"), plse, *_heads(q, *shape, "q"), _TYPE_IDS[q.dtype], q_heads,

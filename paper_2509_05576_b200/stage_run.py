@@ -5,7 +5,9 @@ time of every repetition.  Meant for profiling and size sweeps:
 
 Stages: gram (ptq_hessian_accumulate), inverse (ptq_prepare_hinv), order (ptq_minmax_grid +
 ptq_sensitivity_order), sweep (ptq_quantize_layer), all (the whole path).  The inputs of a stage are produced by
-running the earlier stages once, so every repetition sees valid data.  An L2-sized buffer is rewritten between
+running the earlier stages once, so every repetition sees valid data.  Two more run the layer in low-bit form: linear8 (the layer's
+n inputs cast to 8-bit floating point and multiplied by its quantized weights, ptq_fp8_quantize + ptq_fp8_matmul) and cache4 (one
+decoding step of `rows` requests with n tokens cached of each, `cols` / 128 key-value heads: ptq_cache_plan, _append, _attention).  An L2-sized buffer is rewritten between
 repetitions.  Prints one JSON line.
 """
 from __future__ import annotations
@@ -22,7 +24,7 @@ from . import workloads as wl
 
 def main(argv=None):
     ap = argparse.ArgumentParser()
-    ap.add_argument("--stage", default="all", choices=["gram", "inverse", "order", "sweep", "all"])
+    ap.add_argument("--stage", default="all", choices=["gram", "inverse", "order", "sweep", "all", "linear8", "cache4"])
     ap.add_argument("--rows", type=int, default=256)
     ap.add_argument("--cols", type=int, default=2304)
     ap.add_argument("--n", type=int, default=4096)
@@ -63,6 +65,36 @@ def main(argv=None):
         ptq.quantize_layer(Wd, bufs.Hinv, bufs.perm, bufs.scale, bufs.zero, args.bits, bufs.codes, bufs.What,
                            bufs.H if want_loss else None, bufs.loss if want_loss else None, ws, st, s)
 
+    def make_linear8():
+        q, sc = ptq.fp8_empty(args.rows, args.cols), torch.empty(-(-args.rows // 128), -(-args.cols // 128), device="cuda")
+        ptq.fp8_quantize(bufs.What, q, sc, st, block_rows=128)
+        x = Xd.T.contiguous().to(torch.bfloat16)
+        qx, sx = ptq.fp8_empty(args.n, args.cols), torch.empty(args.n, -(-args.cols // 128), device="cuda")
+        y = torch.empty(args.n, args.rows, dtype=torch.bfloat16, device="cuda")
+
+        def linear8():
+            ptq.fp8_quantize(x, qx, sx, st, stream=s)
+            ptq.fp8_matmul(y, qx, sx, q, sc, st, stream=s)
+        return linear8
+
+    def make_cache4():
+        heads, dim, page, batch = max(1, args.cols // 128), 128, 64, args.rows
+        per = -(-(args.n + 1) // page)
+        cache = ptq.Cache4(batch * per, page, heads, dim)
+        cache.pages.random_(0, 100)                              # any codes; grids are finite positive numbers
+        i32 = dict(dtype=torch.int32, device="cuda")
+        table = torch.arange(batch * per, **i32).view(batch, per)
+        lens, new, free = torch.full((batch,), args.n, **i32), torch.ones(batch, **i32), torch.arange(batch * per, **i32).flip(0).contiguous()
+        slots, positions, cu, after, taken = (torch.empty(c, **i32) for c in (batch, batch, batch + 1, batch, 1))
+        q, k, v = (torch.randn(batch, h, dim, device="cuda").to(torch.bfloat16) for h in (4 * heads, heads, heads))
+        out = torch.empty_like(q)
+
+        def cache4():
+            ptq.cache_plan(lens, new, table, free, page, slots, positions, cu, after, taken, st, stream=s)
+            ptq.cache_append(cache, k, v, slots, st, stream=s)
+            ptq.cache_attention(out, q, cache, table, after, cu, 1, dim ** -0.5, ws, st, stream=s)
+        return cache4
+
     stages = {"gram": gram, "inverse": inverse, "order": order, "sweep": sweep}
 
     def whole():
@@ -72,7 +104,8 @@ def main(argv=None):
     whole()                     # produces the inputs of every stage
     torch.cuda.synchronize()
     ptq.check_status(st, "set-up")
-    fn = whole if args.stage == "all" else stages[args.stage]
+    makers = {"linear8": make_linear8, "cache4": make_cache4}
+    fn = whole if args.stage == "all" else makers[args.stage]() if args.stage in makers else stages[args.stage]
     times = []
     for it in range(args.warmup + args.iters):
         flush.fill_(it & 0xFF)

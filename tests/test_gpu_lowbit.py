@@ -122,7 +122,8 @@ def _check_product(C, A, sa, B, sb):
 
 
 PRODUCTS = [(1, 1, 1), (1, 128, 128), (1, 1000, 2048), (1, 4096, 1024), (2, 130, 129), (15, 256, 384), (16, 64, 4096), (17, 300, 500), (33, 129, 700),
-            (64, 512, 2304), (65, 257, 1000), (128, 256, 128), (200, 1000, 1000), (333, 1000, 2048), (1, 256, 11008), (5, 384, 2200)]
+            (64, 512, 2304), (65, 257, 1000), (128, 256, 128), (200, 1000, 1000), (333, 1000, 2048), (1, 256, 11008), (5, 384, 2200), (3, 20000, 256),
+            (66, 9000, 200)]
 
 
 @pytest.mark.parametrize("m,n,k", PRODUCTS)
@@ -655,6 +656,63 @@ def test_a_captured_step_is_replayed_with_other_lengths():
     for l in (layer, eager):
         ptq.check_status(l.status)
     assert lens == [22, 22, 22, 22]
+
+
+def test_a_cache_beyond_32_bits_of_bytes():
+    page, heads, dim = 1024, 8, 128
+    num_pages = (9 << 29) // (page * heads * 144)                  # 4.5 GiB
+    cache = ptq.Cache4(num_pages, page, heads, dim)
+    g = _gen(5)
+    k, v = torch.randn(40, heads, dim, generator=g), torch.randn(40, heads, dim, generator=g)
+    slots = torch.cat([torch.arange(20), (num_pages - 1) * page + 1000 + torch.arange(20)]).to(torch.int32).cuda()
+    st = ptq.new_status()
+    ptq.cache_append(cache, k.cuda(), v.cuda(), slots, st)
+    kb, vb = torch.empty(40, heads, dim, device="cuda"), torch.empty(40, heads, dim, device="cuda")
+    ptq.cache_read(cache, slots, kb, vb, st)
+    assert np.array_equal(kb.cpu().double().numpy(), ref.held4(k.double().numpy()))
+    c = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    for new in (1, 20):                                            # the last page's tokens from 1000 on, reached by window
+        q = torch.randn(new, 16, dim, generator=g).to(torch.float16)
+        out = torch.empty(new, 16, dim, dtype=torch.float16, device="cuda")
+        ptq.cache_attention(out, q.cuda(), cache, c([[num_pages - 1]]), c([1020]), c([0, new]), new, 0.1, ptq.Workspace(), st, window=1)
+        want = vb[40 - new:].repeat_interleave(2, 1)               # a window of one: the row's own value, times 1 rounded to fp16 and back
+        assert (out.float() - want).abs().max() <= 2.0 ** -10 * float(want.abs().max())
+    ptq.check_status(st)
+
+
+def test_nothing_to_do():
+    st = ptq.new_status()
+    e = lambda *s, t=torch.bfloat16: torch.empty(s, dtype=t, device="cuda")  # noqa: E731
+    ints = lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda")  # noqa: E731
+    ptq.fp8_quantize(e(0, 100), ptq.fp8_empty(0, 100), e(0, 1, t=torch.float32), st)
+    q, s = _cast(torch.randn(3, 128, device="cuda"), 128, st)
+    ptq.fp8_matmul(e(0, 3), ptq.fp8_empty(0, 128), e(0, 1, t=torch.float32), q, s, st)
+    cache, ws = ptq.Cache4(2, 16, 2, 64), ptq.Workspace()
+    ptq.cache_append(cache, e(0, 2, 64), e(0, 2, 64), ints(0), st)
+    ptq.cache_read(cache, ints(0), e(0, 2, 64), e(0, 2, 64), st)
+    ptq.cache_attention(e(0, 4, 64), e(0, 4, 64), cache, ints(2, 3), ints(2), ints(3), 1, 0.1, ws, st)
+    ptq.cache_attention(e(0, 4, 64), e(0, 4, 64), cache, ints(0, 3), ints(0), ints(1), 0, 0.1, ws, st)
+    for rows in (1, 30):                                           # rows of a request that has no page at all
+        out = torch.full((rows, 4, 64), 5.0, dtype=torch.bfloat16, device="cuda")
+        lse = torch.full((rows, 4), 5.0, device="cuda")
+        cu = torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+        ptq.cache_attention(out, torch.ones_like(out), cache, ints(1, 0), ints(1), cu, rows, 0.1, ws, st, lse=lse, causal=False)
+        assert (out == 0).all() and torch.isneginf(lse).all()
+    ptq.check_status(st)
+
+
+def test_two_streams_with_workspaces_of_their_own():
+    lens, new = [3000, 900, 40], [1, 20, 3]
+    want = [_attend(lens, new, 8, 2, 64, 32, torch.bfloat16, seed=s, check=False) for s in (21, 22)]
+    streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], [None, None]
+    for _ in range(3):
+        for i, s in enumerate(streams):
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                got[i] = _attend(lens, new, 8, 2, 64, 32, torch.bfloat16, seed=21 + i, check=False)
+        torch.cuda.synchronize()
+        for i in range(2):
+            assert torch.equal(got[i][0], want[i][0]) and torch.equal(got[i][1], want[i][1])
 
 
 def test_binding_refuses_shared_memory_and_mixed_shapes():
