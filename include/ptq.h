@@ -245,6 +245,7 @@ int ptq_gemm_nt_sliced(double *C, int64_t ldc, const double *A, int64_t lda, con
  * this file hold here too; what these calls add to them:
  *   - `type` parameters name the element type of the caller's activations (ptq_type).
  *   - Calls with nothing to do (no rows, no tokens) return PTQ_OK and launch nothing.
+ *   - A request's table holds at most 2^30 tokens (max_pages * page_size; PTQ_ERR_UNSUPPORTED beyond).
  *   - An output that shares memory with an input, with the workspace or with another output is refused (PTQ_ERR_INVALID_ARG).
  *   - Sizes that live on the device (lengths, offsets, page and slot numbers) are checked there: an entry that is out of range is
  *     recorded in `status` (PTQ_ERR_INVALID_ARG, index = request or token) and is never used as an address.

@@ -305,7 +305,7 @@ int ptq_cache_plan(const int32_t* kv_lens, const int32_t* new_tokens, int batch,
         touch_any(pos, lens, fresh, pages, cu, after, count) || touch_any(cu, lens, fresh, pages, after, count) ||
         touch_any(after, lens, fresh, pages, count) || touch_any(count, lens, fresh, pages))
         return PTQ_ERR_INVALID_ARG;                     // every CTA reads what one of them writes for all
-    if (shift < 0 || (int64_t)max_pages * page_size > 0x7fffffffll) return PTQ_ERR_UNSUPPORTED;
+    if (shift < 0 || (int64_t)max_pages * page_size > (1ll << 30)) return PTQ_ERR_UNSUPPORTED;
     CachePlan p{kv_lens, new_tokens, batch, block_table, ld_table, max_pages, free_pages, num_free, shift, slots, positions, max_tokens,
                 cu_q, kv_lens_out, taken, status};
     const int grid = max_tokens > kPlanTokens ? (int)(((int64_t)max_tokens + kPlanTokens - 1) / kPlanTokens) : 1;
@@ -366,7 +366,7 @@ int ptq_cache_attention(void* out, int64_t o_token, int64_t o_head, float* lse, 
     if (batch == 0 || total_q == 0 || max_q == 0) return PTQ_OK;
     if (!out || !q || !kv_lens || !cu_q || (max_pages > 0 && !block_table) || o_token < head_dim || o_head < head_dim || q_token < 0 || q_head < 0)
         return PTQ_ERR_INVALID_ARG;
-    if ((int64_t)max_pages * page_size > 0x7fffffffll || (int64_t)total_q * q_heads > 0x7fffffffll) return PTQ_ERR_UNSUPPORTED;
+    if ((int64_t)max_pages * page_size > (1ll << 30) || (int64_t)total_q * q_heads > 0x7fffffffll) return PTQ_ERR_UNSUPPORTED;
     if (!aligned16(ws)) return PTQ_ERR_ALIGNMENT;
     if (!ws || ws_bytes < ptq_cache_attention_workspace_bytes(q_heads, kv_heads, head_dim, batch, total_q, max_q)) return PTQ_ERR_WORKSPACE;
     const Span result = heads_span(out, total_q, o_token, q_heads, o_head, head_dim, 2), sums{lse, (size_t)total_q * q_heads * 4},

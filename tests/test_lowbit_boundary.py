@@ -118,7 +118,7 @@ def test_plan_refuses_bad_arguments(ptq):
     for i, name in enumerate(outs):                     # every output lies apart from the inputs and the other outputs
         for other in ins + outs[:i]:
             assert call(**{name: ok[other]}) == ptq.ERR_INVALID_ARG, (name, other)
-    for kw in (dict(page=8), dict(page=24), dict(page=2048), dict(max_pages=1 << 28, ldt=1 << 28)):
+    for kw in (dict(page=8), dict(page=24), dict(page=2048), dict(max_pages=1 << 28, ldt=1 << 28), dict(max_pages=(1 << 26) + 1, ldt=1 << 27)):
         assert call(**kw) == ptq.ERR_UNSUPPORTED, kw
 
 
