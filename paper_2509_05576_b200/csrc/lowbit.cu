@@ -264,7 +264,7 @@ int ptq_fp8_matmul(void* C, int c_type, int64_t ldc, const uint8_t* A, int64_t l
     if (m == 0 || n == 0) return PTQ_OK;
     if (!C || !A || !B || !scale_a || !scale_b || ldc < n || lda < k || ldb < k || ld_scale_a < kb || ld_scale_b < kb)
         return PTQ_ERR_INVALID_ARG;
-    if (k > 0x7fffff00 || (int64_t)cdiv(m, 16) > 65535 || (int64_t)cdiv(n, 128) > 65535) return PTQ_ERR_UNSUPPORTED;
+    if (k > 0x7fffff00 || m > 1 << 20 || n > 1 << 22) return PTQ_ERR_UNSUPPORTED;
     if (!aligned16(A) || !aligned16(B) || lda % 16 || ldb % 16) return PTQ_ERR_ALIGNMENT;
     if (touch_any(rows_span(C, m, ldc, n, type_size(c_type)), rows_span(A, m, lda, k, 1), rows_span(B, n, ldb, k, 1),
                   rows_span(scale_a, m, ld_scale_a, kb, 4), rows_span(scale_b, cdiv(n, kF8Block), ld_scale_b, kb, 4)))

@@ -658,6 +658,47 @@ def test_a_captured_step_is_replayed_with_other_lengths():
     assert lens == [22, 22, 22, 22]
 
 
+def test_captured_prompts_are_replayed_with_other_lengths():
+    """Single tokens and prompts in one captured batch: the launches stay, what they find on the device changes."""
+    page, heads, kv, dim, batch, most, max_pages = 16, 8, 2, 64, 4, 90, 40
+    cache = ptq.Cache4(batch * max_pages, page, kv, dim)
+    g, st, ws = _gen(31), ptq.new_status(), ptq.Workspace()
+    slots = torch.arange(batch * max_pages * page, dtype=torch.int32, device="cuda")
+    kk = torch.randn(slots.numel(), kv, dim, generator=g).cuda()
+    ptq.cache_append(cache, kk, kk.flip(0), slots, st)
+    table = torch.randperm(batch * max_pages, generator=g).to(torch.int32).view(batch, max_pages).cuda()
+    lens, cu = torch.zeros(batch, dtype=torch.int32, device="cuda"), torch.zeros(batch + 1, dtype=torch.int32, device="cuda")
+    q = torch.randn(batch * most, heads, dim, generator=g).to(torch.bfloat16).cuda()
+    out, lse = torch.empty_like(q), torch.empty(batch * most, heads, device="cuda")
+
+    def step(o, l):
+        ptq.cache_attention(o, q, cache, table, lens, cu, most, 0.125, ws, st, lse=l)
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step(out, lse)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step(out, lse)
+    for have, new in (([90, 90, 90, 90], [90, 90, 90, 90]), ([640, 1, 300, 77], [1, 1, 80, 4]), ([5, 0, 17, 639], [5, 0, 1, 90]), ([1, 1, 1, 1], [1, 1, 1, 1]),
+                      ([0, 0, 0, 0], [0, 0, 0, 0]), ([200, 640, 33, 400], [30, 2, 33, 1])):
+        lens.copy_(torch.tensor(have, dtype=torch.int32))
+        cu.copy_(torch.tensor([0] + list(np.cumsum(new)), dtype=torch.int32))
+        out.fill_(9.0)
+        lse.fill_(9.0)
+        want, want_lse = out.clone(), lse.clone()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        step(want, want_lse)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(lse, want_lse)
+        n = sum(new)
+        assert (out[n:] == 9.0).all() and (lse[n:] == 9.0).all() and torch.isfinite(out[:n].float()).all()
+    ptq.check_status(st)
+
+
 def test_a_cache_beyond_32_bits_of_bytes():
     page, heads, dim = 1024, 8, 128
     num_pages = (9 << 29) // (page * heads * 144)                  # 4.5 GiB

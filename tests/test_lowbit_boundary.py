@@ -98,7 +98,7 @@ def test_product_refuses_bad_arguments(ptq):
         assert call(**kw) == ptq.ERR_INVALID_ARG, kw
     for kw in (dict(A=ODD), dict(B=ODD), dict(lda=200), dict(ldb=201)):
         assert call(**kw) == ptq.ERR_ALIGNMENT, kw
-    assert call(m=(1 << 20) + 1) == ptq.ERR_UNSUPPORTED and call(n=1 << 23, ldc=1 << 23) == ptq.ERR_UNSUPPORTED
+    assert call(m=(1 << 20) + 1) == ptq.ERR_UNSUPPORTED and call(n=(1 << 22) + 1, ldc=1 << 23) == ptq.ERR_UNSUPPORTED
     assert call(m=0, C=None, A=None) == ptq.OK and call(n=0) == ptq.OK
 
 
