@@ -5,8 +5,9 @@ n 2^-23 of the sum of their magnitudes, whatever the order (each addition is off
 of a partial sum, which the sum of magnitudes bounds).  The rounding to the output type is half a step of it.
 Attention: a score is off by at most d = (dim + 4) 2^-23 max |q| |k| |scale| (the sum, the factor and their product), and the
 exponential by 2^-22 relative (ex2.approx is good to 2 units in the last place); a probability is then off by e = 2 d + 2^-21
-relative (numerator and sum), enters the second product rounded to fp16 (2^-11 relative, or 2^-25 2^-15 of the largest one below
-its normal range) and the output is off by (e + 2^-11 + n 2^-23) sum p |v| plus the rounding of the type.
+relative (numerator and sum), enters the second product rounded to fp16 (2^-11 relative; below the normal range half a step is
+2^-25, where the largest probability stands at 2^8 or more: 2^-33 of it) and the output is off by (e + 2^-11 + n 2^-23) sum p |v|
+plus n 2^-33 max |v| plus the rounding of the type.
 """
 import numpy as np
 import pytest
@@ -430,7 +431,7 @@ def _attend(lens, new, heads, kv_heads, dim, page, dtype, causal=True, window=0,
             e = (2 * d + 2.0 ** -21)[..., None]
             tol = (e + 2.0 ** -11 + max(n, 1) * 2.0 ** -23) * mass + HALF_STEP[dtype] * np.abs(want) + TINY[dtype]
             if n:
-                tol = tol + n * 2.0 ** -40 * np.abs(vals[i]).max()
+                tol = tol + n * 2.0 ** -33 * np.abs(vals[i]).max()
             off = np.abs(got[at] - want)
             assert (off <= tol).all(), (i, float((off - tol).max()))
             if lse is not None:
