@@ -303,8 +303,8 @@ size_t ptq_cache_page_bytes(int page_size, int kv_heads, int head_dim);
  * Where the new tokens of a batch of requests go: extends the requests' block tables by pages of the free list and lists slot and
  * position of every new token, in one launch.
  *   kv_lens     [batch] int32: tokens cached of each request;  new_tokens [batch] int32: how many are added (0 is fine)
- *   block_table [batch x max_pages] int32, in/out, row stride ld_table: the pages of each request in order.  The entries of pages
- *               that hold cached tokens are read, those of pages that begin with a new token are written, others stay.
+ *   block_table [batch x max_pages] int32, in/out, row stride ld_table: the pages of each request in order.  The entry of a page
+ *               that new tokens fill up is read, those of pages that begin with a new token are written, others stay.
  *   free_pages  [num_free] int32: pages are taken from its front, in the order of the requests and of their pages
  *   slots       [max_tokens] int32, out;  positions [max_tokens] int32, out: of the new tokens of request 0, then 1, ...; -1 in both
  *               behind the last token, which ptq_cache_append skips (a batch padded to a fixed size, as a captured graph needs it)
@@ -346,6 +346,7 @@ int ptq_cache_read(const void *pages, int num_pages, int page_size, int kv_heads
  *           read as fp16 either way, and bf16 queries are brought to fp16 by a power of two for each row, which loses nothing
  *   lse     [total_q][q_heads] float32, or NULL
  *   block_table, kv_lens, cu_q: as ptq_cache_plan leaves them (kv_lens_out).  Rows behind cu_q[batch] are left as they are.
+ *           With a window, the entries of pages whose tokens all lie below the first row's window may be anything.
  *   scale   any number up to 2e38 in magnitude
  *   max_q   the most rows that any request has (it chooses kernels and the workspace; any bound is right, a tight one is fast)
  * Scores, their maximum and sum, and the output are held in float32; the probabilities enter the second product as fp16.

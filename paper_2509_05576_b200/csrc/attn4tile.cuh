@@ -416,7 +416,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn4_tile_kernel(Attn4 a, Ti
             const int j0 = (q.range.chunk0 + c) * kTileKeys, per = a.cache.page_shift - 4;
             auto tile_of = [&](int j) -> const uint8_t* {
                 const int tl = j >> 4;
-                if (tl * kC4Tile >= q.range.hi_any) return nullptr;            // no token there that any row sees
+                // no token there that any row sees: below the window there may be no page any more
+                if (tl * kC4Tile >= q.range.hi_any || tl * kC4Tile + kC4Tile <= q.range.lo_any) return nullptr;
                 int page = a.table[(int64_t)q.b * a.ldt + (tl >> per)];
                 if (page < 0 || page >= a.cache.num_pages) { report(a.status, PTQ_ERR_INVALID_ARG, q.b, 2); page = 0; }
                 return c4_tile<HD>(a.cache, page, q.head, tl & ((1 << per) - 1));

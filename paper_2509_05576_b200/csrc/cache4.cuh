@@ -571,7 +571,11 @@ __global__ void __launch_bounds__(32 * few_warps(NT), 1) attn4_few_kernel(Attn4 
         if (lane < count) {
             const int tl = tile0 + lane, per = a.cache.page_shift - 4;
             int page = a.table[(int64_t)p.b * a.ldt + (tl >> per)];
-            if (page < 0 || page >= a.cache.num_pages) { report(a.status, PTQ_ERR_INVALID_ARG, p.b, 2); page = 0; }
+            if (page < 0 || page >= a.cache.num_pages) {
+                // below the window there may be no page any more: some page's tokens, which are masked, stand in for them
+                if (tl * kC4Tile + kC4Tile > p.lo_any) report(a.status, PTQ_ERR_INVALID_ARG, p.b, 2);
+                page = 0;
+            }
             bulk_load(ring_w + stage * F::chunk_bytes + lane * kTileBytes, c4_tile<HD>(a.cache, page, p.head, tl & ((1 << per) - 1)), kTileBytes, bar);
         }
         ++asked;
