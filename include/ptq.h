@@ -347,7 +347,7 @@ int ptq_cache_read(const void *pages, int num_pages, int page_size, int kv_heads
  *   lse     [total_q][q_heads] float32, or NULL
  *   block_table, kv_lens, cu_q: as ptq_cache_plan leaves them (kv_lens_out).  Rows behind cu_q[batch] are left as they are.
  *           With a window, the entries of pages whose tokens all lie below the first row's window may be anything.
- *   scale   any number up to 2e38 in magnitude
+ *   scale   any number up to 2e38 in magnitude; scores, and scale times the largest |q| of a row, have to lie within float32
  *   max_q   the most rows that any request has (it chooses kernels and the workspace; any bound is right, a tight one is fast)
  * Scores, their maximum and sum, and the output are held in float32; the probabilities enter the second product as fp16.
  * Workspace: ptq_cache_attention_workspace_bytes(q_heads, kv_heads, head_dim, batch, total_q, max_q) (host function, no CUDA

@@ -167,6 +167,11 @@ __device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t (&r)[16])
           "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
+__device__ __forceinline__ void tc_st8(uint32_t taddr, const uint32_t (&r)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
+}
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // Loads that stay where they are written: a chunk's are issued before the wait for room, a whole chunk ahead of their use.
@@ -241,6 +246,31 @@ __device__ __forceinline__ float tile_probs(uint32_t s_tmem, float mult, float o
         tc_st16(s_tmem + ch * 16, w);
     }
     return (part[0].x + part[0].y) + (part[1].x + part[1].y);
+}
+
+// An exponent is (score mult + off), off = 8 - reference mult: one operation for two of them, but off is rounded, by up to half a step of
+// its own.  Up to kTileFar that is a quarter at most, and 2^15.25 an fp16 number still; beyond, the reference is taken from the score
+// before the factor is applied.  Rare, so short rather than fast: a third copy of the loop above, never entered, made everything slower
+// (1024 and 633 tokens behind 7168 and 4430: 229 -> 240 us).
+constexpr float kTileFar = 4194304.f;
+__device__ __noinline__ float tile_probs_far(uint32_t s_tmem, float mult, float ref, int lo, int hi) {
+    float sum = 0.f;
+#pragma unroll 1
+    for (int ch = 0; ch < 8; ++ch) {
+        uint32_t r[16], w[8];
+        tc_ld16(s_tmem + ch * 16, r);
+        tc_wait_ld();
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+            const int j = ch * 16 + e;
+            const float v0 = j >= lo && j < hi ? exp2_approx(fmaf(__uint_as_float(r[e]) - ref, mult, kTilePShift)) : 0.f;
+            const float v1 = j + 1 >= lo && j + 1 < hi ? exp2_approx(fmaf(__uint_as_float(r[e + 1]) - ref, mult, kTilePShift)) : 0.f;
+            sum += v0 + v1;
+            w[e >> 1] = pack_half2(v0, v1);
+        }
+        tc_st8(s_tmem + ch * 8, w);
+    }
+    return sum;
 }
 
 template <typename T, int HD>
@@ -348,7 +378,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn4_tile_kernel(Attn4 a, Ti
             }
             int lo = 0, hi = 0;
             if (live) attn_range(a, p.r, i, lo, hi);
-            float ref = live ? -INFINITY : 0.f, sum = 0.f;       // rows that do not exist see nothing and need no reference
+            // ref: a score, before its factor; rows that do not exist see nothing and need none
+            float ref = live ? -INFINITY : 0.f, sum = 0.f, off = kTilePShift;
+            bool far = false;
             for (int c = p.from; c < p.to; ++c) {
                 ok = __all_sync(0xffffffffu, mbar_wait_bounded(s_full(t), s_phase, abort_flag));
                 if (!ok) break;
@@ -356,12 +388,12 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn4_tile_kernel(Attn4 a, Ti
                 tc_fence_after();
                 const int j0 = (p.range.chunk0 + c) * kTileKeys;
                 const bool whole = j0 >= p.range.lo_all && j0 + kTileKeys <= p.range.hi_all;
-                float top = (whole ? tile_max<true>(s_tmem, 0, 0) : tile_max<false>(s_tmem, lo - j0, hi - j0));
-                top *= mult;
-                const bool move = top > ref + kTileSlack || (ref == -INFINITY && top > ref);
+                const float top = (whole ? tile_max<true>(s_tmem, 0, 0) : tile_max<false>(s_tmem, lo - j0, hi - j0));
+                const bool move = top > ref && (top - ref) * mult > kTileSlack;             // infinite from -infinity
                 if (__any_sync(0xffffffffu, move)) {
-                    const float f = move ? exp2_approx(ref - top) : 1.f;      // 0 from -infinity
-                    if (move) { ref = top; sum *= f; }
+                    const float f = move ? exp2_approx((ref - top) * mult) : 1.f;             // 0 from -infinity
+                    if (move) { ref = top; sum *= f; off = kTilePShift - top * mult; }
+                    far = __any_sync(0xffffffffu, fabsf(off) > kTileFar);
                     if (c > p.from) {
 #pragma unroll
                         for (int ch = 0; ch < HD / 16; ++ch) {
@@ -374,8 +406,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn4_tile_kernel(Attn4 a, Ti
                         }
                     }
                 }
-                const float off = kTilePShift - (ref == -INFINITY ? 0.f : ref);
-                sum += whole ? tile_probs<true>(s_tmem, mult, off, 0, 0) : tile_probs<false>(s_tmem, mult, off, lo - j0, hi - j0);
+                if (far) sum += tile_probs_far(s_tmem, mult, ref == -INFINITY ? 0.f : ref, whole ? 0 : lo - j0, whole ? kTileKeys : hi - j0);
+                else sum += whole ? tile_probs<true>(s_tmem, mult, off, 0, 0) : tile_probs<false>(s_tmem, mult, off, lo - j0, hi - j0);
                 tc_wait_st();
                 tc_fence_before();
                 mbar_arrive(p_full(t));
@@ -386,6 +418,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn4_tile_kernel(Attn4 a, Ti
             o_phase ^= 1u;
             tc_fence_after();
             const bool complete = p.from == 0 && p.to == p.range.chunks;
+            ref = ref == -INFINITY ? ref : ref * mult;
             const float inv = sum == 0.f ? 0.f : 1.f / sum, base_ref = ref == -INFINITY ? 0.f : ref;
             T* out = static_cast<T*>(a.out) + (int64_t)(p.r.row0 + i) * a.o_token + (int64_t)qh * a.o_head;
             float* slot = a.partial + (2 * blockIdx.x + (p.from == 0)) * tile_partial_floats(HD);

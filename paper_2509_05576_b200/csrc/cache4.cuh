@@ -709,20 +709,26 @@ __global__ void __launch_bounds__(32 * few_warps(NT), 1) attn4_few_kernel(Attn4 
             uint32_t pf[NT][kFewTiles][2];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                float off[2];
-#pragma unroll
-                for (int h = 0; h < 2; ++h) off[h] = kAttnPShift - (m[nt][h] == -INFINITY ? 0.f : m[nt][h] * mult[nt][h]);
+                // The difference comes before the factor: a product of the reference is off by up to half a step of its own, more
+                // than fp16 has room for once scores pass 2^23.  Two at a time this costs what one fused operation each does.
+                const float2 factor = make_float2(mult[nt][0], mult[nt][1]), shift = make_float2(kAttnPShift, kAttnPShift);
+                const float2 minus_ref = make_float2(m[nt][0] == -INFINITY ? 0.f : -m[nt][0], m[nt][1] == -INFINITY ? 0.f : -m[nt][1]);
+                float2 part = make_float2(0.f, 0.f);
 #pragma unroll
                 for (int tl = 0; tl < kFewTiles; ++tl) {
                     float pr[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        pr[e] = exp2_approx(fmaf(x[nt][tl][e], mult[nt][e & 1], off[e & 1]));
-                        l[nt][e & 1] += pr[e];
+                    for (int e = 0; e < 4; e += 2) {
+                        const float2 y = fma2(add2(make_float2(x[nt][tl][e], x[nt][tl][e + 1]), minus_ref), factor, shift);
+                        pr[e] = exp2_approx(y.x);
+                        pr[e + 1] = exp2_approx(y.y);
+                        part = add2(part, make_float2(pr[e], pr[e + 1]));
                     }
                     pf[nt][tl][0] = transpose8(pack_half2(pr[0], pr[1]));
                     pf[nt][tl][1] = transpose8(pack_half2(pr[2], pr[3]));
                 }
+                l[nt][0] += part.x;
+                l[nt][1] += part.y;
             }
 #pragma unroll
             for (int tl = 0; tl < kFewTiles; ++tl) {
