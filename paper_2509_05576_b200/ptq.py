@@ -174,18 +174,56 @@ def _rowmajor(t, name):
     return t.stride(0)
 
 
+def _is_capturing(dev, stream):
+    """Whether what a call puts on `stream` (None: the current one of device `dev`) becomes part of a CUDA graph."""
+    if dev < 0:
+        return False
+    if torch._C._cuda_getDevice() != dev:
+        with torch.cuda.device(dev):
+            return _is_capturing(dev, stream)
+    if stream is None or stream.cuda_stream == torch._C._cuda_getCurrentRawStream(dev):
+        return torch._C._cuda_isCurrentStreamCapturing()
+    with torch.cuda.stream(stream):
+        return torch._C._cuda_isCurrentStreamCapturing()
+
+
 class Workspace:
-    """A growable device scratch buffer handed to the library calls."""
+    """A growable device scratch buffer handed to the library calls.
+
+    A call that needs more than there is gets a larger buffer, and the old one goes back to the allocator, unless a call that was
+    being captured has used it: a graph writes to the buffer it was captured with at every replay, so that one stays as long as
+    the workspace does.  Keep the workspace for as long as the graph is replayed.  Buffers belong to the stream of the call that
+    made them, and the allocator is told of every other stream that uses them."""
 
     def __init__(self, device="cuda"):
         self.device = torch.device(device)
-        self.buf = None
+        self.buf, self._dev = None, -1
+        self._captured = []           # buffers that some graph writes to
+        self._streams = ()            # raw streams that the allocator knows to use `buf`
 
-    def get(self, nbytes: int):
+    def get(self, nbytes: int, stream=None):
+        """At least `nbytes`, for a call on `stream` (None: the current one of the workspace's device)."""
         if self.buf is None or self.buf.numel() < nbytes:
-            self.buf = None
-            self.buf = torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=self.device)
-        return self.buf
+            self._grow(int(nbytes), stream)
+        buf, dev = self.buf, self._dev
+        if dev >= 0:
+            raw = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+            if raw not in self._streams:
+                buf.record_stream(torch.cuda.current_stream(dev) if stream is None else stream)
+                self._streams += (raw,)
+        if _is_capturing(dev, stream) and not any(b is buf for b in self._captured):
+            self._captured.append(buf)
+        return buf
+
+    def _grow(self, nbytes, stream):
+        self.buf = None
+        if stream is None:
+            self.buf = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=self.device)
+        else:
+            with torch.cuda.stream(stream):
+                self.buf = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=self.device)
+        self._dev = dev = self.buf.get_device()
+        self._streams = () if dev < 0 else (torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream,)
 
 
 def new_status(device="cuda"):
@@ -213,7 +251,7 @@ def hessian_accumulate(H, X, ws, status, stream=None, f64=False):
         raise ValueError("H must be contiguous [cols, cols]")
     fn = lib().ptq_hessian_accumulate_f64 if f64 else lib().ptq_hessian_accumulate
     need = workspace_bytes(CALL_HESSIAN_ACCUMULATE_F64 if f64 else CALL_HESSIAN_ACCUMULATE, 0, cols, n)
-    buf = ws.get(need)
+    buf = ws.get(need, stream)
     _check(fn(_ptr(H), _ptr(X), cols, n, ldx, _ptr(buf), buf.numel(), _ptr(status), _stream(stream)),
            "ptq_hessian_accumulate")
 
@@ -234,7 +272,7 @@ def hessian_accumulate_conv(H, act, kh, kw, stride, pad, ws, status, stream=None
     cols, n = conv_unfolded_shape(act.shape, kh, kw, stride, pad)
     if H.shape != (cols, cols) or not H.is_contiguous():
         raise ValueError("H must be contiguous [channels kh kw, channels kh kw]")
-    buf = ws.get(workspace_bytes(CALL_HESSIAN_ACCUMULATE, 0, cols, n))
+    buf = ws.get(workspace_bytes(CALL_HESSIAN_ACCUMULATE, 0, cols, n), stream)
     _check(lib().ptq_hessian_accumulate_conv(_ptr(H), _ptr(act), b, c, h, w, int(kh), int(kw), int(stride), int(pad),
                                              _ptr(buf), buf.numel(), _ptr(status), _stream(stream)),
            "ptq_hessian_accumulate_conv")
@@ -244,7 +282,7 @@ def prepare_hinv(H, damp, damp_mode, Hinv, Hinv_diag, lambda_out, ws, status, st
     """Hinv = (H + lambda I)^-1 (Sec. 5 item 1); also its diagonal and lambda (device scalars)."""
     _dev(H, torch.float64, "H"); _dev(Hinv, torch.float64, "Hinv")
     cols = H.shape[0]
-    buf = ws.get(workspace_bytes(CALL_PREPARE_HINV, 0, cols, 0))
+    buf = ws.get(workspace_bytes(CALL_PREPARE_HINV, 0, cols, 0), stream)
     _check(lib().ptq_prepare_hinv(_ptr(H), cols, int(damp_mode), float(damp), _ptr(Hinv), _ptr(Hinv_diag),
                                   _ptr(lambda_out), _ptr(buf), buf.numel(), _ptr(status), _stream(stream)),
            "ptq_prepare_hinv")
@@ -261,7 +299,7 @@ def sensitivity_order(W, Hinv_diag, scale, zero, bits, score_mode, S, perm, ws, 
     """Sec. 4.2 steps 1-3: column scores S and the descending, stable column order perm."""
     _dev(W, torch.float32, "W")
     rows, cols = W.shape
-    buf = ws.get(workspace_bytes(CALL_SENSITIVITY_ORDER, rows, cols, 0))
+    buf = ws.get(workspace_bytes(CALL_SENSITIVITY_ORDER, rows, cols, 0), stream)
     _check(lib().ptq_sensitivity_order(_ptr(W), rows, cols, _rowmajor(W, "W"), _ptr(Hinv_diag), _ptr(scale),
                                        _ptr(zero), int(bits), int(score_mode), _ptr(S), _ptr(perm), _ptr(buf),
                                        buf.numel(), _ptr(status), _stream(stream)), "ptq_sensitivity_order")
@@ -291,7 +329,7 @@ def gemm_nt_sliced(C, A, B, alpha, ws, status, b_is_kn=False, stream=None):
     _dev(C, torch.float64, "C"); _dev(A, torch.float64, "A"); _dev(B, torch.float64, "B")
     m, k = A.shape
     n = B.shape[1] if b_is_kn else B.shape[0]
-    buf = ws.get(int(lib().ptq_gemm_nt_sliced_workspace_bytes(m, n, k)))
+    buf = ws.get(int(lib().ptq_gemm_nt_sliced_workspace_bytes(m, n, k)), stream)
     _check(lib().ptq_gemm_nt_sliced(_ptr(C), _rowmajor(C, "C"), _ptr(A), _rowmajor(A, "A"), _ptr(B), _rowmajor(B, "B"),
                                     1 if b_is_kn else 0, m, n, k, float(alpha), _ptr(buf), buf.numel(), _ptr(status),
                                     _stream(stream)), "ptq_gemm_nt_sliced")
@@ -299,14 +337,14 @@ def gemm_nt_sliced(C, A, B, alpha, ws, status, b_is_kn=False, stream=None):
 
 def selftest_wait_timeout(which, limit_cycles, ws, status, stream=None):
     """Makes one of the library's bounded device-side waits run out (0: grid barrier, 1: sweep counter)."""
-    buf = ws.get(256)
+    buf = ws.get(256, stream)
     _check(lib().ptq_selftest_wait_timeout(int(which), int(limit_cycles), _ptr(buf), buf.numel(), _ptr(status),
                                            _stream(stream)), "ptq_selftest_wait_timeout")
 
 
 def selftest_abandoned_sweep(limit_cycles, ws, status, stream=None):
     """Has the sweep wait for a factorisation that never finishes; the sweep's abort word afterwards (device scalar)."""
-    buf, word = ws.get(ABANDONED_SWEEP_BYTES), torch.zeros(1, dtype=torch.int32, device=status.device)
+    buf, word = ws.get(ABANDONED_SWEEP_BYTES, stream), torch.zeros(1, dtype=torch.int32, device=status.device)
     _check(lib().ptq_selftest_abandoned_sweep(int(limit_cycles), _ptr(buf), buf.numel(), _ptr(word), _ptr(status),
                                               _stream(stream)), "ptq_selftest_abandoned_sweep")
     return word
@@ -334,7 +372,7 @@ def quantize_layer(W, Hinv, perm, scale, zero, bits, codes, What, H_undamped, lo
     _dev(W, torch.float32, "W"); _dev(Hinv, torch.float64, "Hinv"); _dev(perm, torch.int32, "perm")
     _dev(codes, torch.uint8, "codes")
     rows, cols = W.shape
-    buf = ws.get(workspace_bytes(CALL_QUANTIZE_LAYER, rows, cols, 0))
+    buf = ws.get(workspace_bytes(CALL_QUANTIZE_LAYER, rows, cols, 0), stream)
     _check(lib().ptq_quantize_layer(_ptr(W), rows, cols, _rowmajor(W, "W"), _ptr(Hinv), _ptr(perm), _ptr(scale),
                                     _ptr(zero), int(bits), _ptr(codes), _ptr(What), _ptr(H_undamped), _ptr(loss_out),
                                     _ptr(buf), buf.numel(), _ptr(status), _stream(stream)), "ptq_quantize_layer")
@@ -346,7 +384,7 @@ def quantize_layer_dynamic(W, Hinv, scale, zero, bits, score_mode, block, codes,
     _dev(W, torch.float32, "W"); _dev(Hinv, torch.float64, "Hinv"); _dev(codes, torch.uint8, "codes")
     _dev(order_out, torch.int32, "order_out")
     rows, cols = W.shape
-    buf = ws.get(workspace_bytes(CALL_QUANTIZE_LAYER_DYNAMIC, rows, cols, 0))
+    buf = ws.get(workspace_bytes(CALL_QUANTIZE_LAYER_DYNAMIC, rows, cols, 0), stream)
     _check(lib().ptq_quantize_layer_dynamic(_ptr(W), rows, cols, _rowmajor(W, "W"), _ptr(Hinv), _ptr(scale), _ptr(zero),
                                             int(bits), int(score_mode), int(block), _ptr(codes), _ptr(What),
                                             _ptr(order_out), _ptr(H_undamped), _ptr(loss_out), _ptr(buf), buf.numel(),
@@ -359,7 +397,7 @@ def quantize_layer_per_row(W, Hinv, scale, zero, bits, score_mode, codes, What, 
     _dev(W, torch.float32, "W"); _dev(Hinv, torch.float64, "Hinv"); _dev(codes, torch.uint8, "codes")
     _dev(perm_rows, torch.int32, "perm_rows")
     rows, cols = W.shape
-    buf = ws.get(workspace_bytes(CALL_QUANTIZE_LAYER_PER_ROW, rows, cols, 0))
+    buf = ws.get(workspace_bytes(CALL_QUANTIZE_LAYER_PER_ROW, rows, cols, 0), stream)
     _check(lib().ptq_quantize_layer_per_row(_ptr(W), rows, cols, _rowmajor(W, "W"), _ptr(Hinv), _ptr(scale), _ptr(zero),
                                             int(bits), int(score_mode), _ptr(codes), _ptr(What), _ptr(perm_rows),
                                             _ptr(H_undamped), _ptr(loss_out), _ptr(buf), buf.numel(), _ptr(status),
@@ -560,7 +598,7 @@ def cache_attention(out, q, cache, block_table, kv_lens, cu_q, max_q, scale, ws,
         plse, ld = _matrix(lse, tokens, q_heads, _F32, dev, "lse")
         _expect(ld == q_heads, "lse must be contiguous")
     need = _attention_workspace_bytes(q_heads, cache.kv_heads, cache.head_dim, batch, tokens, max_q)
-    buf = ws.get(need)
+    buf = ws.get(need, stream)
     _expect(buf.get_device() == dev, f"the workspace is on {buf.device}, the tensors are on cuda:{dev}")
     _call(lib().ptq_cache_attention, dev, stream, *_heads(out, *shape, "out"), plse, *_heads(q, *shape, "q"), _TYPE_IDS[q.dtype], q_heads,
           *cache._args(dev), table, ldt, max_pages, _vector(kv_lens, batch, dev, "kv_lens"), _vector(cu_q, batch + 1, dev, "cu_q"), batch,

@@ -72,3 +72,88 @@ def test_scores_of_any_size(power, new, n):
             assert (np.abs(got[i, h] - want) <= (2.0 ** -11 + n * 2.0 ** -23 + 2.0 ** -20) * mass + 2.0 ** -8 * np.abs(want)).all()
             exact = float(x.max()) * abs(scale) + np.log(len(best))
             assert abs(got_lse[i, h] - exact) <= 2.0 ** -21 * (2 + abs(exact))
+
+
+class _Attention:
+    """Attention of the last tokens of a few requests, sized so that more rows need a larger workspace."""
+
+    def __init__(self, seed):
+        self.heads, self.dim, page, n = 8, 64, 16, 700
+        g = base._gen(seed)
+        self.n, self.cache, self.st = n, ptq.Cache4(-(-n // page), page, 2, self.dim), ptq.new_status()
+        x = torch.randn(n, 2, self.dim, generator=g).cuda()
+        ptq.cache_append(self.cache, x, x.flip(0), _c(np.arange(n)), self.st)
+        self.table, self.lens = _c([np.arange(-(-n // page))]), _c([n])
+        self.q = torch.randn(300, self.heads, self.dim, generator=g).to(torch.float16).cuda()
+
+    def __call__(self, out, new, ws, stream=None):
+        ptq.cache_attention(out, self.q[:new], self.cache, self.table, self.lens, self.cu[new], new, 0.125, ws, self.st, stream=stream)
+
+    def outputs(self, *news):
+        self.cu = {n: _c([0, n]) for n in news}
+        return [torch.full((n, self.heads, self.dim), 7.0, dtype=torch.float16, device="cuda") for n in news]
+
+
+def test_a_captured_call_keeps_its_scratch_when_others_need_more():
+    job, ws = _Attention(1), ptq.Workspace()
+    few, many, want = job.outputs(1, 300, 1)
+    job(want, 1, ptq.Workspace())
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        job(few, 1, ws)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        job(few, 1, ws)
+    first, size = ws.buf.data_ptr(), ws.buf.numel()
+    job(many, 300, ws)
+    assert ws.buf.numel() > size and ws.buf.data_ptr() != first
+    others = [torch.full((size,), 0x5A, dtype=torch.uint8, device="cuda") for _ in range(4)]       # the freed buffer's size
+    assert all(o.data_ptr() != first for o in others)
+    for _ in range(3):
+        few.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(few, want) and all((o == 0x5A).all() for o in others)
+    ptq.check_status(job.st)
+
+
+def test_scratch_of_another_stream_is_not_given_away_while_it_is_used():
+    job = _Attention(2)
+    few, many, want, want_many = job.outputs(1, 300, 1, 300)
+    job(want, 1, ptq.Workspace())
+    job(want_many, 300, ptq.Workspace())
+    ws, side = ptq.Workspace(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(50_000_000)                              # some 25 ms in which nothing of what follows runs there
+    job(few, 1, ws, stream=side)
+    size, first = ws.buf.numel(), ws.buf.data_ptr()
+    job(many, 300, ws, stream=side)                                # a larger buffer: the first one is free for `side` alone
+    others = [torch.full((size,), 0x5A, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    assert all(o.data_ptr() != first for o in others) and not side.query()
+    used = ws.buf.data_ptr(), ws.buf.numel()
+    del ws
+    others += [torch.full((used[1],), 0x5A, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    assert all(o.data_ptr() != used[0] for o in others)
+    torch.cuda.synchronize()
+    ptq.check_status(job.st)
+    assert torch.equal(few, want) and torch.equal(many, want_many) and all((o == 0x5A).all() for o in others)
+
+
+def test_scratch_made_on_one_stream_and_used_on_another_is_not_given_away():
+    job, ws = _Attention(3), ptq.Workspace()
+    few, want = job.outputs(1, 1)
+    job(want, 1, ws)                                               # made on the current stream
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(50_000_000)
+    job(few, 1, ws, stream=side)
+    size, first = ws.buf.numel(), ws.buf.data_ptr()
+    del ws
+    others = [torch.full((size,), 0x5A, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    assert all(o.data_ptr() != first for o in others) and not side.query()
+    torch.cuda.synchronize()
+    assert torch.equal(few, want) and all((o == 0x5A).all() for o in others)
