@@ -323,6 +323,10 @@ int ptq_cache_append(void* pages, int num_pages, int page_size, int kv_heads, in
     if (tokens < 0 || !type_size(type)) return PTQ_ERR_INVALID_ARG;
     if (tokens == 0) return PTQ_OK;
     if (!k || !v || !slots || k_token < 0 || k_head < 0 || v_token < 0 || v_head < 0) return PTQ_ERR_INVALID_ARG;
+    const Span all{pages, (size_t)num_pages * ptq_cache_page_bytes(page_size, kv_heads, head_dim)}, at{slots, (size_t)tokens * 4};
+    if (touch_any(all, heads_span(k, tokens, k_token, kv_heads, k_head, head_dim, type_size(type)),
+                  heads_span(v, tokens, v_token, kv_heads, v_head, head_dim, type_size(type)), at))
+        return PTQ_ERR_INVALID_ARG;
     return cache_tokens(true, c, head_dim,
                         C4Tokens{const_cast<void*>(k), const_cast<void*>(v), k_token, k_head, v_token, v_head, slots, tokens, 0, status},
                         type, static_cast<cudaStream_t>(stream_));
