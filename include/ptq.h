@@ -246,7 +246,9 @@ int ptq_gemm_nt_sliced(double *C, int64_t ldc, const double *A, int64_t lda, con
  *   - `type` parameters name the element type of the caller's activations (ptq_type).
  *   - Calls with nothing to do (no rows, no tokens) return PTQ_OK and launch nothing.
  *   - A request's table holds at most 2^30 tokens (max_pages * page_size; PTQ_ERR_UNSUPPORTED beyond).
- *   - An output that shares memory with an input, with the workspace or with another output is refused (PTQ_ERR_INVALID_ARG).
+ *   - An output that shares memory with an input, with the workspace or with another output is refused (PTQ_ERR_INVALID_ARG), and so
+ *     is one whose own rows overlap.  What counts are all bytes from an array's first to its last; only rows of heads with the same
+ *     strides (q and out of ptq_cache_attention, k and v of ptq_cache_read) may alternate in one buffer.
  *   - Sizes that live on the device (lengths, offsets, page and slot numbers) are checked there: an entry that is out of range is
  *     recorded in `status` (PTQ_ERR_INVALID_ARG, index = request or token) and is never used as an address.
  * ------------------------------------------------------------------------------------------------------------------
@@ -330,8 +332,7 @@ int ptq_cache_append(void *pages, int num_pages, int page_size, int kv_heads, in
                      int64_t k_head, const void *v, int64_t v_token, int64_t v_head, int type, const int32_t *slots, int tokens,
                      int32_t *status, void *stream);
 
-/* The values that the cache holds at `slots`, to k and v (as above, written; their elements may alternate in one buffer, but must
- * differ); rows of negative slots are left as they are. */
+/* The values that the cache holds at `slots`, to k and v (as above, written); rows of negative slots are left as they are. */
 int ptq_cache_read(const void *pages, int num_pages, int page_size, int kv_heads, int head_dim, void *k, int64_t k_token,
                    int64_t k_head, void *v, int64_t v_token, int64_t v_head, int type, const int32_t *slots, int tokens,
                    int32_t *status, void *stream);

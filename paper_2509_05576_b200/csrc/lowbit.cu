@@ -35,6 +35,30 @@ Span rows_span(const void* p, int64_t rows, int64_t ld, int64_t cols, int size) 
 Span heads_span(const void* p, int64_t tokens, int64_t ld_token, int64_t heads, int64_t ld_head, int64_t dim, int size) {
     return {p, tokens > 0 ? (size_t)((tokens - 1) * ld_token + (heads - 1) * ld_head + dim) * size : 0};
 }
+// Whether two sets of rows [tokens][heads] of `width` bytes with the same strides (of at least that), the second `d` bytes behind
+// the first, share a byte; `self`: whether two different rows of one set do.
+bool rows_meet(int64_t d, int64_t tokens, int64_t heads, int64_t by_token, int64_t by_head, int64_t width, bool self) {
+    if (self && (by_token >= (heads - 1) * by_head + width || by_head >= (tokens - 1) * by_token + width)) return false;      // one inside the other
+    for (int64_t j = -(heads - 1); j <= heads - 1; ++j) {
+        const int64_t x = d + j * by_head;                // row i of the second set begins x + i by_token behind some row of the first
+        const int64_t down = -(x / by_token) - (x % by_token > 0);
+        for (int64_t i = down; i <= down + 1; ++i) {
+            const int64_t gap = x + i * by_token;
+            if (i > -tokens && i < tokens && gap > -width && gap < width && !(self && i == 0 && j == 0)) return true;
+        }
+    }
+    return false;
+}
+struct Rows { const void* p; int64_t tokens, by_token, heads, by_head, dim; int size; };
+Span span_of(const Rows& r) { return heads_span(r.p, r.tokens, r.by_token, r.heads, r.by_head, r.dim, r.size); }
+bool meets_itself(const Rows& r) { return rows_meet(0, r.tokens, r.heads, r.by_token * r.size, r.by_head * r.size, r.dim * r.size, true); }
+// Rows of one shape may alternate in a buffer (the parts of a fused projection); with other strides whole spans are compared.
+bool meet(const Rows& a, const Rows& b) {
+    if (!touch(span_of(a), span_of(b))) return false;
+    if (a.by_token != b.by_token || a.by_head != b.by_head || a.heads != b.heads || a.size != b.size || b.by_token < b.dim) return true;
+    return rows_meet(static_cast<const char*>(b.p) - static_cast<const char*>(a.p), a.tokens, a.heads, a.by_token * a.size, a.by_head * a.size,
+                     a.dim * a.size, false);
+}
 
 int page_shift_of(int page_size) {
     for (int s = 4; s <= 10; ++s)
@@ -341,8 +365,8 @@ int ptq_cache_read(const void* pages, int num_pages, int page_size, int kv_heads
     if (tokens == 0) return PTQ_OK;
     if (!k || !v || !slots || k_token < head_dim || k_head < head_dim || v_token < head_dim || v_head < head_dim) return PTQ_ERR_INVALID_ARG;
     const Span all{pages, (size_t)num_pages * ptq_cache_page_bytes(page_size, kv_heads, head_dim)}, at{slots, (size_t)tokens * 4};
-    if (touch_any(heads_span(k, tokens, k_token, kv_heads, k_head, head_dim, type_size(type)), all, at) ||
-        touch_any(heads_span(v, tokens, v_token, kv_heads, v_head, head_dim, type_size(type)), all, at))
+    const Rows kr{k, tokens, k_token, kv_heads, k_head, head_dim, type_size(type)}, vr{v, tokens, v_token, kv_heads, v_head, head_dim, type_size(type)};
+    if (touch_any(span_of(kr), all, at) || touch_any(span_of(vr), all, at) || meets_itself(kr) || meets_itself(vr) || meet(kr, vr))
         return PTQ_ERR_INVALID_ARG;
     return cache_tokens(false, c, head_dim, C4Tokens{k, v, k_token, k_head, v_token, v_head, slots, tokens, 0, status}, type,
                         static_cast<cudaStream_t>(stream_));
@@ -373,13 +397,13 @@ int ptq_cache_attention(void* out, int64_t o_token, int64_t o_head, float* lse, 
     if ((int64_t)max_pages * page_size > (1ll << 30) || (int64_t)total_q * q_heads > 0x7fffffffll) return PTQ_ERR_UNSUPPORTED;
     if (!aligned16(ws)) return PTQ_ERR_ALIGNMENT;
     if (!ws || ws_bytes < ptq_cache_attention_workspace_bytes(q_heads, kv_heads, head_dim, batch, total_q, max_q)) return PTQ_ERR_WORKSPACE;
-    const Span result = heads_span(out, total_q, o_token, q_heads, o_head, head_dim, 2), sums{lse, (size_t)total_q * q_heads * 4},
-               scratch{ws, ptq_cache_attention_workspace_bytes(q_heads, kv_heads, head_dim, batch, total_q, max_q)},
-               rows = heads_span(q, total_q, q_token, q_heads, q_head, head_dim, 2),
+    const Rows orows{out, total_q, o_token, q_heads, o_head, head_dim, 2}, qrows{q, total_q, q_token, q_heads, q_head, head_dim, 2};
+    const Span result = span_of(orows), sums{lse, (size_t)total_q * q_heads * 4},
+               scratch{ws, ptq_cache_attention_workspace_bytes(q_heads, kv_heads, head_dim, batch, total_q, max_q)}, rows = span_of(qrows),
                all{pages, (size_t)num_pages * ptq_cache_page_bytes(page_size, kv_heads, head_dim)},
                table = rows_span(block_table, max_pages > 0 ? batch : 0, ld_table, max_pages, 4), lens{kv_lens, (size_t)batch * 4},
                cu{cu_q, (size_t)batch * 4 + 4};
-    if (touch_any(result, sums, scratch, rows, all, table, lens, cu) || touch_any(sums, scratch, rows, all, table, lens, cu) ||
+    if (meet(orows, qrows) || meets_itself(orows) || touch_any(result, sums, scratch, all, table, lens, cu) || touch_any(sums, scratch, rows, all, table, lens, cu) ||
         touch_any(scratch, rows, all, table, lens, cu))
         return PTQ_ERR_INVALID_ARG;
     DeviceState* dev = nullptr;

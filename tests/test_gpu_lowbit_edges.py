@@ -157,3 +157,26 @@ def test_scratch_made_on_one_stream_and_used_on_another_is_not_given_away():
     assert all(o.data_ptr() != first for o in others) and not side.query()
     torch.cuda.synchronize()
     assert torch.equal(few, want) and all((o == 0x5A).all() for o in others)
+
+
+def test_rows_of_one_shape_may_alternate_in_a_buffer():
+    heads, kv, dim, page, n = 8, 2, 64, 16, 90
+    g = base._gen(5)
+    cache, st = ptq.Cache4(6, page, kv, dim), ptq.new_status()
+    x = torch.randn(n, kv, dim, generator=g).cuda()
+    ptq.cache_append(cache, x, x.flip(0), _c(np.arange(n)), st)
+    both = torch.full((n, kv, 2, dim), 9.0, device="cuda")
+    apart = [torch.empty(n, kv, dim, device="cuda") for _ in range(2)]
+    ptq.cache_read(cache, _c(np.arange(n)), both[:, :, 0], both[:, :, 1], st)
+    ptq.cache_read(cache, _c(np.arange(n)), *apart, st)
+    assert torch.equal(both[:, :, 0], apart[0]) and torch.equal(both[:, :, 1], apart[1])
+    args = cache, _c([np.arange(6)]), _c([n]), _c([0, 40]), 40, 0.125, ptq.Workspace(), st
+    q = torch.randn(40, heads, dim, generator=g).to(torch.bfloat16).cuda()
+    want = torch.empty_like(q)
+    ptq.cache_attention(want, q, *args)
+    for shape, part in (((40, 2, heads, dim), lambda t, i: t[:, i]), ((40, heads, 2, dim), lambda t, i: t[:, :, i]), ((heads, 40, 2, dim), lambda t, i: t[:, :, i].transpose(0, 1))):
+        buf = torch.full(shape, 9.0, dtype=torch.bfloat16, device="cuda")
+        part(buf, 0).copy_(q)
+        ptq.cache_attention(part(buf, 1), part(buf, 0), *args)
+        assert torch.equal(part(buf, 1), want) and torch.equal(part(buf, 0), q)
+    ptq.check_status(st)
