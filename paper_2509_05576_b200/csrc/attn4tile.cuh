@@ -177,17 +177,17 @@ __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sy
 // Loads that stay where they are written: a chunk's are issued before the wait for room, a whole chunk ahead of their use.
 __device__ __forceinline__ uint4 ld_global16(const uint8_t* p) {
     uint4 v;
-    asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
     return v;
 }
 __device__ __forceinline__ uint32_t ld_global4(const uint8_t* p) {
     uint32_t v;
-    asm volatile("ld.global.nc.u32 %0, [%1];" : "=r"(v) : "l"(p));
+    asm volatile("ld.global.u32 %0, [%1];" : "=r"(v) : "l"(p));
     return v;
 }
 __device__ __forceinline__ uint32_t ld_global2(const uint8_t* p) {
     uint16_t v;
-    asm volatile("ld.global.nc.u16 %0, [%1];" : "=h"(v) : "l"(p));
+    asm volatile("ld.global.u16 %0, [%1];" : "=h"(v) : "l"(p));
     return v;
 }
 
@@ -343,7 +343,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn4_tile_kernel(Attn4 a, Ti
                 uint4 raw[HD / 8];                       // the whole row at once: one trip to memory
                 if (live && a.q_vec) {
 #pragma unroll
-                    for (int c = 0; c < HD / 8; ++c) raw[c] = __ldg(reinterpret_cast<const uint4*>(q) + c);
+                    for (int c = 0; c < HD / 8; ++c) raw[c] = reinterpret_cast<const uint4*>(q)[c];
                 } else {
 #pragma unroll
                     for (int c = 0; c < HD / 8; ++c) {

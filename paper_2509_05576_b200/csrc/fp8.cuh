@@ -29,13 +29,15 @@ template <> __device__ __forceinline__ float from_f32(float x) { return x; }
 template <> __device__ __forceinline__ __half from_f32(float x) { return __float2half_rn(x); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f32(float x) { return __float2bfloat16_rn(x); }
 
-// Eight consecutive values of which `n` exist (the others become 0); vec: p is 16-byte aligned.
+// Eight consecutive values of which `n` exist (the others become 0); vec: p is 16-byte aligned.  Plain loads, here and in all kernels of
+// this kind: they are put in place while the kernel before them may still write what they read (chained_begin), and the read-only
+// path (__ldg, const __restrict__) is for memory that nobody writes while a kernel lives.  Times are the same.
 template <typename T>
-__device__ __forceinline__ void load8(const T* __restrict__ p, int n, bool vec, float (&v)[8]) {
+__device__ __forceinline__ void load8(const T* p, int n, bool vec, float (&v)[8]) {
     if (vec && n >= 8) {
         alignas(16) T t[8];
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(t)[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(t)[i] = reinterpret_cast<const uint4*>(p)[i];
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = to_f32<T>(t[i]);
     } else {
@@ -98,8 +100,8 @@ constexpr uint32_t kF8NanCodes = 0x7f7f7f7fu;
 // 16-bit inputs are bound by the instructions between them (8192 x 4096: float32 28 us, 5.9 TB/s; bf16 24 us, 4.3 TB/s).  A block a half warp: two or four
 // in a row were slower (26.8, 30.8, 33.4 us with one, two, four).
 template <typename T>
-__global__ void __launch_bounds__(256) f8_quantize_rows_kernel(const T* __restrict__ x, int rows, int cols, int64_t ldx, int vec,
-                                                                uint8_t* __restrict__ q, int64_t ldq, float* __restrict__ scale,
+__global__ void __launch_bounds__(256) f8_quantize_rows_kernel(const T* x, int rows, int cols, int64_t ldx, int vec,
+                                                                uint8_t* q, int64_t ldq, float* scale,
                                                                 int64_t lds, int32_t* status) {
     chained_begin();
     // two blocks of eight rows: a warp's two half warps take neighbouring blocks
@@ -126,8 +128,8 @@ __global__ void __launch_bounds__(256) f8_quantize_rows_kernel(const T* __restri
 
 // One scale per block of 128 x 128: a CTA holds the block in registers (64 values a thread), so x is read once.
 template <typename T>
-__global__ void __launch_bounds__(256) f8_quantize_blocks_kernel(const T* __restrict__ x, int rows, int cols, int64_t ldx, int vec,
-                                                                  uint8_t* __restrict__ q, int64_t ldq, float* __restrict__ scale,
+__global__ void __launch_bounds__(256) f8_quantize_blocks_kernel(const T* x, int rows, int cols, int64_t ldx, int vec,
+                                                                  uint8_t* q, int64_t ldq, float* scale,
                                                                   int64_t lds, int32_t* status) {
     chained_begin();
     __shared__ float warp_top[8];
@@ -340,18 +342,18 @@ f8_product_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constan
             float now[4], ahead[4];
             auto scales = [&](int b) {
                 if (sa_vec && b + 4 <= p.kb) {
-                    const float4 f = __ldg(reinterpret_cast<const float4*>(sa + b));
+                    const float4 f = *reinterpret_cast<const float4*>(sa + b);
                     ahead[0] = f.x; ahead[1] = f.y; ahead[2] = f.z; ahead[3] = f.w;
                 } else {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) ahead[j] = b + j < p.kb ? __ldg(sa + b + j) : 0.f;
+                    for (int j = 0; j < 4; ++j) ahead[j] = b + j < p.kb ? sa[b + j] : 0.f;
                 }
             };
             scales(0);
 #pragma unroll 1
             for (int b0 = 0; b0 < p.kb && ok; b0 += 4) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) now[j] = ahead[j] * (b0 + j < p.kb ? __ldg(sb + b0 + j) : 0.f);
+                for (int j = 0; j < 4; ++j) now[j] = ahead[j] * (b0 + j < p.kb ? sb[b0 + j] : 0.f);
                 if (b0 + 4 < p.kb) scales(b0 + 4);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -494,7 +496,7 @@ f8_product_few_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_con
 #pragma unroll
             for (int i = 0; i < per; ++i) {
                 const int e = t + 128 * i, r = row0 + e / kF8ScaleBlocks, bb = b + e % kF8ScaleBlocks;
-                ahead[i] = r < p.m && bb < b1 ? __ldg(p.sa + (int64_t)r * p.ldsa + bb) * __ldg(sb + bb) : 0.f;
+                ahead[i] = r < p.m && bb < b1 ? p.sa[(int64_t)r * p.ldsa + bb] * sb[bb] : 0.f;
             }
         };
 #pragma unroll
