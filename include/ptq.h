@@ -262,7 +262,8 @@ typedef enum { PTQ_F32 = 0, PTQ_F16 = 1, PTQ_BF16 = 2 } ptq_type;
  * A power of two makes the quotient exact, so that a code is one rounding of x.
  *   x       [rows x cols] of x_type, row stride ldx (16-byte loads are used where base and stride allow)
  *   block_rows  1 (activations: a scale per row and 128 columns) or 128 (weights: a scale per 128 x 128)
- *   q       [rows x cols] bytes, out, row stride ldq, a multiple of 16; bytes behind a row's last column are left as they are
+ *   q       [rows x cols] bytes, out, row stride ldq, a multiple of 16 (that of a single row may be any); bytes behind a row's last
+ *           column are left as they are
  *   scale   [ceil(rows / block_rows) x ceil(cols / 128)] float32, out, row stride ld_scale
  * A NaN or an infinity is recorded in `status` (PTQ_ERR_NONFINITE, index = row, or first row of the block); its block's codes and
  * scale become NaN, and with them what a product makes of that row (or of those columns).
@@ -278,7 +279,8 @@ int ptq_fp8_quantize(const void *x, int x_type, int rows, int cols, int64_t ldx,
  *   C       [m x n] of c_type, out, row stride ldc
  *   A       [m x k] bytes, row stride lda;  scale_a [m x ceil(k / 128)], row stride ld_scale_a
  *   B       [n x k] bytes (a weight matrix as the layer stores it), row stride ldb;  scale_b [ceil(n / 128) x ceil(k / 128)]
- *   lda, ldb: multiples of 16 (PTQ_ERR_ALIGNMENT otherwise); what lies behind a row's last column is not read
+ *   lda, ldb: multiples of 16 (PTQ_ERR_ALIGNMENT otherwise; that of a single row may be any); what lies behind a row's last column
+ *           is not read
  * Few rows (a decoded token) are bound by the one read of B; no workspace.  Beyond m = 2^20 or n = 2^22: PTQ_ERR_UNSUPPORTED.
  */
 int ptq_fp8_matmul(void *C, int c_type, int64_t ldc, const uint8_t *A, int64_t lda, const float *scale_a, int64_t ld_scale_a,

@@ -258,7 +258,7 @@ int ptq_fp8_quantize(const void* x, int x_type, int rows, int cols, int64_t ldx,
     if (rows == 0) return PTQ_OK;
     if (!x || !q || !scale || ldx < cols || ldq < cols || ld_scale < kb) return PTQ_ERR_INVALID_ARG;
     if (rows > 0x7fffff00 || cols > 0x7fffff00 || (block_rows > 1 ? cdiv(rows, kF8Block) : cdiv(kb, 2)) > 65535) return PTQ_ERR_UNSUPPORTED;
-    if (!aligned16(q) || ldq % 16) return PTQ_ERR_ALIGNMENT;
+    if (!aligned16(q) || (rows > 1 && ldq % 16)) return PTQ_ERR_ALIGNMENT;
     const Span in = rows_span(x, rows, ldx, cols, size), codes = rows_span(q, rows, ldq, cols, 1),
                factors = rows_span(scale, cdiv(rows, block_rows), ld_scale, kb, 4);
     if (touch_any(codes, in, factors) || touch(factors, in)) return PTQ_ERR_INVALID_ARG;
@@ -289,6 +289,8 @@ int ptq_fp8_matmul(void* C, int c_type, int64_t ldc, const uint8_t* A, int64_t l
     if (!C || !A || !B || !scale_a || !scale_b || ldc < n || lda < k || ldb < k || ld_scale_a < kb || ld_scale_b < kb)
         return PTQ_ERR_INVALID_ARG;
     if (k > 0x7fffff00 || m > 1 << 20 || n > 1 << 22) return PTQ_ERR_UNSUPPORTED;
+    if (m == 1) lda = ((int64_t)k + 15) / 16 * 16;       // the stride of a single row is never used, but a tensor map has one
+    if (n == 1) ldb = ((int64_t)k + 15) / 16 * 16;
     if (!aligned16(A) || !aligned16(B) || lda % 16 || ldb % 16) return PTQ_ERR_ALIGNMENT;
     if (touch_any(rows_span(C, m, ldc, n, type_size(c_type)), rows_span(A, m, lda, k, 1), rows_span(B, n, ldb, k, 1),
                   rows_span(scale_a, m, ld_scale_a, kb, 4), rows_span(scale_b, cdiv(n, kF8Block), ld_scale_b, kb, 4)))

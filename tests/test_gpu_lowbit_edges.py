@@ -180,3 +180,20 @@ def test_rows_of_one_shape_may_alternate_in_a_buffer():
         ptq.cache_attention(part(buf, 1), part(buf, 0), *args)
         assert torch.equal(part(buf, 1), want) and torch.equal(part(buf, 0), q)
     ptq.check_status(st)
+
+
+@pytest.mark.parametrize("k", [1, 100, 129, 5000])
+def test_a_single_row_has_no_stride(k):
+    """Contiguous operands of one row, of any length: the stride of a single row is never used."""
+    x, w = torch.randn(1, k, generator=base._gen(k)).cuda(), torch.randn(1, k, generator=base._gen(k + 1)).cuda()
+    st, got = ptq.new_status(), []
+    for t, rows in ((x, 1), (w, 128)):
+        q, s = torch.empty(1, k, dtype=torch.float8_e4m3fn, device="cuda"), torch.empty(1, -(-k // 128), device="cuda")
+        ptq.fp8_quantize(t, q, s, st, block_rows=rows)
+        rq, rs = ref.f8_cast(t.cpu().double().numpy(), rows)
+        assert np.array_equal(q.cpu().double().numpy(), rq) and np.array_equal(s.cpu().double().numpy(), rs)
+        got += [q, s]
+    C = torch.empty(1, 1, device="cuda")
+    ptq.fp8_matmul(C, *got, st)
+    ptq.check_status(st)
+    base._check_product(C, *got)
