@@ -197,3 +197,78 @@ def test_a_single_row_has_no_stride(k):
     ptq.fp8_matmul(C, *got, st)
     ptq.check_status(st)
     base._check_product(C, *got)
+
+
+def test_calls_wait_for_copies_and_for_other_streams():
+    """The kernels are put in place early; what a copy, another stream's work or an ordinary kernel before them wrote has to be there."""
+    m, k = 4096, 2048
+    st = ptq.new_status()
+    x, q, s = torch.zeros(m, k, device="cuda"), ptq.fp8_empty(m, k), torch.empty(m, k // 128, device="cuda")
+    hosts = [torch.randn(m, k, generator=base._gen(i)).pin_memory() for i in range(3)]
+    want = []
+    for h in hosts:
+        ptq.fp8_quantize(h.cuda(), q, s, st)
+        want.append((q.view(torch.uint8).clone(), s.clone()))
+    side, got = torch.cuda.Stream(), []
+    for i, h in enumerate(hosts * 2):
+        qq, ss = ptq.fp8_empty(m, k), torch.empty(m, k // 128, device="cuda")
+        ptq.fp8_quantize(x, q, s, st)                              # puts its successor in place early
+        if i < 3:
+            x.copy_(h, non_blocking=True)
+        else:
+            side.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(side):
+                torch.cuda._sleep(2_000_000)
+                x.copy_(h, non_blocking=True)
+            torch.cuda.current_stream().wait_stream(side)
+        ptq.fp8_quantize(x, qq, ss, st)
+        got.append((qq, ss))
+    torch.cuda.synchronize()
+    ptq.check_status(st)
+    for i, (qq, ss) in enumerate(got):
+        assert torch.equal(qq.view(torch.uint8), want[i % 3][0]) and torch.equal(ss, want[i % 3][1]), i
+
+
+def test_a_capture_that_forks_and_joins():
+    """Casts, products and attention on two streams of one captured graph, replayed with other inputs."""
+    heads, kv, dim, page, n = 8, 2, 64, 16, 500
+    st, g = ptq.new_status(), base._gen(8)
+    cache = ptq.Cache4(40, page, kv, dim)
+    cache.pages.zero_()
+    x = torch.randn(n, kv, dim, generator=g).cuda()
+    ptq.cache_append(cache, x, x.flip(0), _c(np.arange(n)), st)
+    B, sb = base._cast(torch.randn(heads * dim, 700, generator=g).cuda(), 128, st)
+    a = torch.zeros(96, 700, dtype=torch.bfloat16, device="cuda")
+    A, sa = ptq.fp8_empty(96, 700), torch.empty(96, 6, device="cuda")
+    q, out = torch.empty(96, heads, dim, dtype=torch.bfloat16, device="cuda"), torch.empty(96, heads, dim, dtype=torch.bfloat16, device="cuda")
+    new = torch.zeros(96, kv, dim, dtype=torch.bfloat16, device="cuda")
+    lens, slots, table, cu, ws = _c([n + 96]), _c(np.arange(n, n + 96)), _c([np.arange(40)]), _c([0, 96]), ptq.Workspace()
+    side, main = torch.cuda.Stream(), torch.cuda.Stream()
+
+    def step(s):
+        side.wait_stream(s)
+        ptq.fp8_quantize(a, A, sa, st, stream=s)
+        ptq.cache_append(cache, new, new, slots, st, stream=side)
+        ptq.fp8_matmul(q.flatten(1), A, sa, B, sb, st, stream=s)
+        s.wait_stream(side)
+        ptq.cache_attention(out, q, cache, table, lens, cu, 96, 0.125, ws, st, stream=s)
+
+    main.wait_stream(torch.cuda.current_stream())
+    step(main)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=main):
+        step(main)
+    for i in range(4):
+        a.copy_(torch.randn(96, 700, generator=g))
+        new.copy_(torch.randn(96, kv, dim, generator=g))
+        out.fill_(7.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        out.fill_(7.0)
+        step(torch.cuda.current_stream())
+        torch.cuda.synchronize()
+        assert torch.equal(got, out) and torch.isfinite(got.float()).all()
+    ptq.check_status(st)
