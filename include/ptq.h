@@ -272,11 +272,13 @@ int ptq_fp8_quantize(const void *x, int x_type, int rows, int cols, int64_t ldx,
                      float *scale, int64_t ld_scale, int32_t *status, void *stream);
 
 /*
- * C = A B^T of operands in 8-bit floating point with block scales, as ptq_fp8_quantize makes them (any float32 scales are taken):
+ * C = A B^T of operands in 8-bit floating point with block scales, as ptq_fp8_quantize makes them (any float32 scales are taken;
+ * the product of a scale_a and a scale_b has to lie within float32 too):
  *     C[i][j] = sum_b scale_a[i][b] scale_b[j / 128][b] sum_{k in block b} A[i][k] B[j][k],    blocks of 128 along k
  * Within a block the products are summed on the tensor cores, the blocks are joined in float32, and the result is rounded once to
  * c_type.
- *   C       [m x n] of c_type, out, row stride ldc
+ *   C       [m x n] of c_type, out, row stride ldc (beyond 64 rows, rows that are multiples of 16 bytes are written up to five times
+ *           as fast)
  *   A       [m x k] bytes, row stride lda;  scale_a [m x ceil(k / 128)], row stride ld_scale_a
  *   B       [n x k] bytes (a weight matrix as the layer stores it), row stride ldb;  scale_b [ceil(n / 128) x ceil(k / 128)]
  *   lda, ldb: multiples of 16 (PTQ_ERR_ALIGNMENT otherwise; that of a single row may be any); what lies behind a row's last column
@@ -346,13 +348,16 @@ int ptq_cache_read(const void *pages, int num_pages, int page_size, int kv_heads
  *     out = sum_j softmax_j(scale q . k_j) v_j,     lse = log sum_j exp(scale q . k_j)
  * A row that sees no key gets out = 0 and lse = -infinity.  Query head h reads key-value head h / (q_heads / kv_heads).
  *   q, out  [total_q][q_heads][head_dim] of `type` (PTQ_F16 or PTQ_BF16), strides between tokens and heads in elements; the cache is
- *           read as fp16 either way, and bf16 queries are brought to fp16 by a power of two for each row, which loses nothing
+ *           read as fp16 either way, and bf16 queries are brought to fp16 by a power of two for each row: values down to 2^-31 of a
+ *           row's largest stay as they are, smaller ones are off by at most 2^-39 of it
  *   lse     [total_q][q_heads] float32, or NULL
  *   block_table, kv_lens, cu_q: as ptq_cache_plan leaves them (kv_lens_out).  Rows behind cu_q[batch] are left as they are.
  *           With a window, the entries of pages whose tokens all lie below the first row's window may be anything.
  *   scale   any number up to 2e38 in magnitude; scores, and scale times the largest |q| of a row, have to lie within float32
  *   max_q   the most rows that any request has (it chooses kernels and the workspace; any bound is right, a tight one is fast)
- * Scores, their maximum and sum, and the output are held in float32; the probabilities enter the second product as fp16.
+ * Scores, their maximum and sum, and the output are held in float32; the probabilities enter the second product as fp16: rounded to
+ * 11 bits, and small ones to within 2^-40 of the row's largest in calls with max_q x q_heads / kv_heads up to 16, to within 2^-33 of it
+ * in others.
  * Workspace: ptq_cache_attention_workspace_bytes(q_heads, kv_heads, head_dim, batch, total_q, max_q) (host function, no CUDA
  * calls; 0 for what is not supported); it does not depend on lengths.
  */

@@ -18,6 +18,8 @@
 // The reference of a row's exponentials is only moved when a score lies more than 2^7 above it (P then still fits fp16), so that O is
 // hardly ever rescaled.
 //
+// 128 registers a thread at launch, dealt out by role; the compiler spills 32 bytes a thread (heads of 128).
+//
 // The units (128 keys of one tile) are dealt to the CTAs in equal shares, as those of the kernel for few rows; what a row tile sees of
 // the keys differs from tile to tile, so a first small kernel lists the tiles with the units before each.
 #pragma once
@@ -26,7 +28,8 @@
 namespace ptq {
 
 constexpr int kTileRows = 256, kTileKeys = 128, kTileThreads = 512, kTileMaxCtas = 160, kScheduleThreads = 1024;
-// What beginning and ending a tile costs a CTA, in chunks.
+// What beginning and ending a tile costs a CTA, in chunks.  With 0, 1, 2 (attention alone, us): six prompts of 1500 tokens, heads of 64
+// 143, 106, 94; two of 1024 tokens behind up to 7168, heads of 128 264, 265, 256.
 constexpr int kTileCost = 1;
 constexpr float kTilePShift = 8.f, kTileSlack = 7.f;     // P = 2^(x - ref + 8) <= 2^15
 
@@ -526,60 +529,60 @@ __global__ void __launch_bounds__(kTileThreads, 1) attn4_tile_kernel(Attn4 a, Ti
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
         if (warp == 12) {
-        // ------------------------------------------------------------ products
-        int stage = 0;
-        uint32_t kv_phase = 0, q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
-        bool ok = true;
-        auto scores = [&](int t, int st) {
-            const uint32_t qa = kF8DescLo + ((base + t * (S::q_bytes / 2)) >> 4), kb = kF8DescLo + ((base + S::q_bytes + st * S::stage_bytes) >> 4);
+            // ------------------------------------------------------------ products
+            int stage = 0;
+            uint32_t kv_phase = 0, q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
+            bool ok = true;
+            auto scores = [&](int t, int st) {
+                const uint32_t qa = kF8DescLo + ((base + t * (S::q_bytes / 2)) >> 4), kb = kF8DescLo + ((base + S::q_bytes + st * S::stage_bytes) >> 4);
 #pragma unroll
-            for (int ks = 0; ks < HD / 16; ++ks) {
-                const uint32_t at = (ks >> 2) * (128 * 128 >> 4) + (ks & 3) * 2;
-                tc_mma_f16(tmem + t * 128, qa + at, kb + at, f16_idesc(kTileKeys), ks > 0);
-            }
-            tc_commit_elected(s_full(t));
-        };
-        while (ok && walk.next(a, list, p)) {
-            const bool two = p.r.n * a.ratio - p.tile * kTileRows > 128;
-            const int tiles = two ? 2 : 1;
-            ok = __all_sync(0xffffffffu, mbar_wait_bounded(kv_full(stage), kv_phase, abort_flag));
-            for (int t = 0; t < tiles && ok; ++t) {
-                ok = __all_sync(0xffffffffu, mbar_wait_bounded(q_full(t), q_phase[t], abort_flag));
-                if (!ok) break;
-                q_phase[t] ^= 1u;
-                tc_fence_after();
-                scores(t, stage);
-            }
-            for (int c = p.from; c < p.to && ok; ++c) {
-                const int next = stage ^ 1;
-                const uint32_t next_phase = kv_phase ^ (stage == 1 ? 1u : 0u);
-                const bool more = c + 1 < p.to;
-                for (int t = 0; t < tiles; ++t) {
-                    ok = __all_sync(0xffffffffu, mbar_wait_bounded(p_full(t), p_phase[t], abort_flag));
-                    if (!ok) break;
-                    p_phase[t] ^= 1u;
-                    tc_fence_after();
-                    const uint32_t vb = kF8DescLo + ((base + S::q_bytes + stage * S::stage_bytes + S::k_bytes) >> 4);
-#pragma unroll
-                    for (int ks = 0; ks < kTileKeys / 16; ++ks)
-                        tc_mma_f16_tmem(tmem + 256 + t * 128, tmem + t * 128 + ks * 8, vb + (ks >> 2) * (HD * 128 >> 4) + (ks & 3) * 2, f16_idesc(HD),
-                                        c > p.from || ks > 0);
-                    if (t == tiles - 1) tc_commit_elected(kv_empty(stage));
-                    if (more) {
-                        if (t == 0) {
-                            ok = __all_sync(0xffffffffu, mbar_wait_bounded(kv_full(next), next_phase, abort_flag));
-                            if (!ok) break;
-                            tc_fence_after();
-                        }
-                        scores(t, next);
-                    } else {
-                        tc_commit_elected(o_full(t));
-                    }
+                for (int ks = 0; ks < HD / 16; ++ks) {
+                    const uint32_t at = (ks >> 2) * (128 * 128 >> 4) + (ks & 3) * 2;
+                    tc_mma_f16(tmem + t * 128, qa + at, kb + at, f16_idesc(kTileKeys), ks > 0);
                 }
-                stage = next;
-                kv_phase = next_phase;
+                tc_commit_elected(s_full(t));
+            };
+            while (ok && walk.next(a, list, p)) {
+                const bool two = p.r.n * a.ratio - p.tile * kTileRows > 128;
+                const int tiles = two ? 2 : 1;
+                ok = __all_sync(0xffffffffu, mbar_wait_bounded(kv_full(stage), kv_phase, abort_flag));
+                for (int t = 0; t < tiles && ok; ++t) {
+                    ok = __all_sync(0xffffffffu, mbar_wait_bounded(q_full(t), q_phase[t], abort_flag));
+                    if (!ok) break;
+                    q_phase[t] ^= 1u;
+                    tc_fence_after();
+                    scores(t, stage);
+                }
+                for (int c = p.from; c < p.to && ok; ++c) {
+                    const int next = stage ^ 1;
+                    const uint32_t next_phase = kv_phase ^ (stage == 1 ? 1u : 0u);
+                    const bool more = c + 1 < p.to;
+                    for (int t = 0; t < tiles; ++t) {
+                        ok = __all_sync(0xffffffffu, mbar_wait_bounded(p_full(t), p_phase[t], abort_flag));
+                        if (!ok) break;
+                        p_phase[t] ^= 1u;
+                        tc_fence_after();
+                        const uint32_t vb = kF8DescLo + ((base + S::q_bytes + stage * S::stage_bytes + S::k_bytes) >> 4);
+#pragma unroll
+                        for (int ks = 0; ks < kTileKeys / 16; ++ks)
+                            tc_mma_f16_tmem(tmem + 256 + t * 128, tmem + t * 128 + ks * 8, vb + (ks >> 2) * (HD * 128 >> 4) + (ks & 3) * 2, f16_idesc(HD),
+                                            c > p.from || ks > 0);
+                        if (t == tiles - 1) tc_commit_elected(kv_empty(stage));
+                        if (more) {
+                            if (t == 0) {
+                                ok = __all_sync(0xffffffffu, mbar_wait_bounded(kv_full(next), next_phase, abort_flag));
+                                if (!ok) break;
+                                tc_fence_after();
+                            }
+                            scores(t, next);
+                        } else {
+                            tc_commit_elected(o_full(t));
+                        }
+                    }
+                    stage = next;
+                    kv_phase = next_phase;
+                }
             }
-        }
         }
     }
     tc_fence_before();

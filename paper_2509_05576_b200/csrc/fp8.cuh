@@ -97,7 +97,7 @@ __device__ __forceinline__ void f8_store8(uint8_t* p, int n, uint2 c) {
 constexpr uint32_t kF8NanCodes = 0x7f7f7f7fu;
 
 // One scale per row and block of 128 columns: sixteen lanes hold a block, eight values each.  One read of x, one write of the codes;
-// 16-bit inputs are bound by the instructions between them (8192 x 4096: float32 28 us, 5.9 TB/s; bf16 24 us, 4.3 TB/s).  A block a half warp: two or four
+// 16-bit inputs are bound by the instructions between them (8192 x 4096: float32 29 us, 5.7 TB/s; bf16 25 us, 4.1 TB/s).  A block a half warp: two or four
 // in a row were slower (26.8, 30.8, 33.4 us with one, two, four).
 template <typename T>
 __global__ void __launch_bounds__(256) f8_quantize_rows_kernel(const T* x, int rows, int cols, int64_t ldx, int vec,
@@ -126,7 +126,8 @@ __global__ void __launch_bounds__(256) f8_quantize_rows_kernel(const T* x, int r
     }
 }
 
-// One scale per block of 128 x 128: a CTA holds the block in registers (64 values a thread), so x is read once.
+// One scale per block of 128 x 128: a CTA holds the block in registers (64 values a thread), so x is read once.  4096 x 11008: float32 39 us
+// (5.8 TB/s); bf16 and fp16 66 us (2.0 TB/s), bound by latency: sixteen warps an SM, and a thread's eight loads follow one another.
 template <typename T>
 __global__ void __launch_bounds__(256) f8_quantize_blocks_kernel(const T* x, int rows, int cols, int64_t ldx, int vec,
                                                                   uint8_t* q, int64_t ldq, float* scale,
@@ -224,9 +225,11 @@ __device__ __forceinline__ void store_row16(T* p, const float* v, int n, bool ve
 // Many rows: tiles of 128 rows of A by 256 of B, persistent.  A TMA warp fills four stages of one k block (48 KB); one thread
 // issues the four MMAs of a block into one of two TMEM buffers; eight epilogue warps drain the other, one row of the tile and
 // 128 columns a thread, and join it to their float32 sums.  128 x 256 x 128 takes the tensor cores 512 clocks; a block takes some
-// 1050 here.  8192 x 11008 x 4096: 375 us (1.97 PFLOP/s), of which 60 to 80 go when the epilogue does nothing and another 60 when
+// 1050 here.  8192 x 11008 x 4096: 394 us replayed one after another (1.88 PFLOP/s; 375 for a single launch at a higher clock, and with
+// its cast 400 to 480 as a program calls it, by the power limit), of which 60 to 80 go when the epilogue does nothing and another 60 when
 // half of B is loaded: 48 KB from L2 for each block of a tile, and the drain of 128 KB of TMEM, hold the tensor cores up in turn.
-// (Pairs of SMs on one tile would load a third less; not built.)
+// (Pairs of SMs on one tile would load a third less; not built.)  A row of C that is no multiple of 16 bytes is stored value by value,
+// 32 rows a warp: 2048 x 4095 x 4096 takes 115 us where 2048 x 4096 x 4096 takes 39, 4000 x 1301 x 1024 91 where 4000 x 1304 x 1024 takes 19.
 constexpr int kF8TileM = 128, kF8TileN = 256, kF8Stages = 4, kF8Threads = 384;
 constexpr int kF8StageBytes = (kF8TileM + kF8TileN) * kF8Block;
 constexpr int kF8SmemBytes = 1024 + kF8Stages * kF8StageBytes + 256;
@@ -272,53 +275,53 @@ f8_product_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constan
     // registers: eight epilogue warps with 128 sums each want more than a third of them
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-    if (warp == 0) {
-        if (lane == 0) {
-            int stage = 0, armed[kF8Stages];
-            uint32_t phase = 0;
+        if (warp == 0) {
+            if (lane == 0) {
+                int stage = 0, armed[kF8Stages];
+                uint32_t phase = 0;
 #pragma unroll
-            for (int s = 0; s < kF8Stages; ++s) armed[s] = -1;
-            bool ok = true;
-            for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
-                int tm, tn;
-                f8_tile(tile, tiles_m, tiles_n, tm, tn);
-                for (int b = 0; b < p.kb; ++b) {
-                    ok = mbar_wait_bounded(empty_bar(stage), phase ^ 1u, abort_flag);
-                    if (!ok) break;
-                    const uint32_t dst = base + stage * kF8StageBytes;
-                    mbar_arrive_expect_tx(full_bar(stage), kF8StageBytes);
-                    armed[stage] = (int)phase;
-                    tma_load_2d(dst, &mapA, b * kF8Block, tm * kF8TileM, full_bar(stage));
-                    tma_load_2d(dst + kF8TileM * kF8Block, &mapB, b * kF8Block, tn * kF8TileN, full_bar(stage));
-                    if (++stage == kF8Stages) { stage = 0; phase ^= 1u; }
+                for (int s = 0; s < kF8Stages; ++s) armed[s] = -1;
+                bool ok = true;
+                for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
+                    int tm, tn;
+                    f8_tile(tile, tiles_m, tiles_n, tm, tn);
+                    for (int b = 0; b < p.kb; ++b) {
+                        ok = mbar_wait_bounded(empty_bar(stage), phase ^ 1u, abort_flag);
+                        if (!ok) break;
+                        const uint32_t dst = base + stage * kF8StageBytes;
+                        mbar_arrive_expect_tx(full_bar(stage), kF8StageBytes);
+                        armed[stage] = (int)phase;
+                        tma_load_2d(dst, &mapA, b * kF8Block, tm * kF8TileM, full_bar(stage));
+                        tma_load_2d(dst + kF8TileM * kF8Block, &mapB, b * kF8Block, tn * kF8TileN, full_bar(stage));
+                        if (++stage == kF8Stages) { stage = 0; phase ^= 1u; }
+                    }
+                }
+                if (!ok) {
+                    for (int s = 0; s < kF8Stages; ++s)
+                        if (armed[s] >= 0) drain_copy(full_bar(s), (uint32_t)armed[s]);
                 }
             }
-            if (!ok) {
-                for (int s = 0; s < kF8Stages; ++s)
-                    if (armed[s] >= 0) drain_copy(full_bar(s), (uint32_t)armed[s]);
-            }
-        }
-    } else if (warp == 1) {
-        int stage = 0, buf = 0;
-        uint32_t phase = 0, acc_phase = 0;
-        bool ok = true;
-        for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
-            for (int b = 0; b < p.kb && ok; ++b) {
-                ok = __all_sync(0xffffffffu, mbar_wait_bounded(acc_empty(buf), acc_phase ^ 1u, abort_flag) &&
-                                                 mbar_wait_bounded(full_bar(stage), phase, abort_flag));
-                if (!ok) break;
-                tc_fence_after();
-                const uint32_t a = kF8DescLo + ((base + stage * kF8StageBytes) >> 4);
+        } else if (warp == 1) {
+            int stage = 0, buf = 0;
+            uint32_t phase = 0, acc_phase = 0;
+            bool ok = true;
+            for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
+                for (int b = 0; b < p.kb && ok; ++b) {
+                    ok = __all_sync(0xffffffffu, mbar_wait_bounded(acc_empty(buf), acc_phase ^ 1u, abort_flag) &&
+                                                     mbar_wait_bounded(full_bar(stage), phase, abort_flag));
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t a = kF8DescLo + ((base + stage * kF8StageBytes) >> 4);
 #pragma unroll
-                for (int ks = 0; ks < 4; ++ks)
-                    tc_mma_f8(tmem + buf * kF8TileN, a + 2 * ks, a + 2 * ks + (kF8TileM * kF8Block >> 4), f8_idesc(kF8TileN), ks > 0);
-                tc_commit_elected(empty_bar(stage));
-                tc_commit_elected(acc_full(buf));
-                if (++stage == kF8Stages) { stage = 0; phase ^= 1u; }
-                if (++buf == 2) { buf = 0; acc_phase ^= 1u; }
+                    for (int ks = 0; ks < 4; ++ks)
+                        tc_mma_f8(tmem + buf * kF8TileN, a + 2 * ks, a + 2 * ks + (kF8TileM * kF8Block >> 4), f8_idesc(kF8TileN), ks > 0);
+                    tc_commit_elected(empty_bar(stage));
+                    tc_commit_elected(acc_full(buf));
+                    if (++stage == kF8Stages) { stage = 0; phase ^= 1u; }
+                    if (++buf == 2) { buf = 0; acc_phase ^= 1u; }
+                }
             }
         }
-    }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         const int quarter = warp & 3, half = (warp - 4) >> 2;
@@ -338,7 +341,7 @@ f8_product_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constan
 #pragma unroll
             for (int c = 0; c < kF8Block; ++c) acc[c] = 0.f;
             // A row's scales come four k blocks at a time and a group ahead: one by one, every lane's load was a sector of its own
-            // for each block (8192 x 11008 x 4096 with its cast: 432 us, 408 so, 400 with two sums an instruction).
+            // for each block (8192 x 11008 x 4096 with its cast, replayed: 432 us, 408 so, 400 with two sums an instruction).
             float now[4], ahead[4];
             auto scales = [&](int b) {
                 if (sa_vec && b + 4 <= p.kb) {

@@ -203,7 +203,12 @@ void attn_tile_launch(const Attn4& a, const TileList& list, int sms, cudaStream_
     }
 }
 
-// Requests with up to this many rows (new tokens x query heads of a kv head) go to the kernel for few rows, others to the tiles.
+// Requests with up to this many rows (new tokens x query heads of a kv head) go to the kernel for few rows, others to the tiles.  Measured
+// with heads of 128, us, few rows / tiles, by rows of a request:
+//   64 requests of up to 2048 tokens, 4 kv heads:  16: 63 / 82;  24: 92 / 82;  32: 98 / 82;  64: 168 / 85;  128: 297 / 90
+//   8 requests of up to 8192 tokens, 8 kv heads:   16: 69 / 68;  24: 69 / 70;  32: 74 / 71;  64: 112 / 73;  128: 191 / 78
+//   1 request of 8192 tokens, 8 kv heads:          16: 85 / 41;  24: 61 / 45;  32: 64 / 50;  64: 63 / 52;   128: 69 / 55
+// A request alone is split so finely that joining its parts costs the kernel for few rows as much as the attention does; batches decide.
 constexpr int kFewRows = 16;
 
 // The pieces of attention's workspace.
