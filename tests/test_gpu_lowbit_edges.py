@@ -272,3 +272,31 @@ def test_a_capture_that_forks_and_joins():
         torch.cuda.synchronize()
         assert torch.equal(got, out) and torch.isfinite(got.float()).all()
     ptq.check_status(st)
+
+
+@pytest.mark.parametrize("eager_first", [True, False])
+def test_scratch_of_a_capture_may_be_made_before_it_or_in_it(eager_first):
+    job, ws = _Attention(4), ptq.Workspace()
+    few, many, want, want_many = job.outputs(1, 300, 1, 300)
+    job(want, 1, ptq.Workspace())
+    job(want_many, 300, ptq.Workspace())
+    if eager_first:
+        job(few, 1, ws)                                            # on the current stream; the capture is on another one
+    torch.cuda.synchronize()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=side):
+        job(few, 1, ws)
+    held = ws.buf.data_ptr()
+    job(many, 300, ws)                                             # grows, eagerly
+    assert ws.buf.data_ptr() != held
+    others = [torch.full((1 << 24,), 0x5A, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    for _ in range(3):
+        few.fill_(7.0)
+        many.fill_(7.0)
+        graph.replay()
+        job(many, 300, ws)
+        torch.cuda.synchronize()
+        assert torch.equal(few, want) and torch.equal(many, want_many) and all((o == 0x5A).all() for o in others)
+    ptq.check_status(job.st)
+    del graph, ws
+    torch.cuda.synchronize()
